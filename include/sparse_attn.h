@@ -389,6 +389,54 @@ int sparse_attn_linear_w8a8(const uint8_t* xq, const float* sx, int64_t ldx, con
                             const float* sw, int64_t ldw, const float* bias, void* y, int64_t ldy,
                             int64_t M, int64_t N, int64_t K, void* stream);
 
+/* Element types of the layer-norm calls. */
+enum { SA_BF16 = 0, SA_F32 = 1 };
+
+/*
+ * Layer norm over the channels of every row:
+ *   y = (x - mean) rstd * w + b,  rstd = 1 / sqrt(var + eps),
+ * var the mean of (x - mean)^2.  The rows form `groups` runs of rows / groups
+ * consecutive rows, each with its own weight and bias (one group: the usual
+ * norm; one per sample: a video DiT's modulated norm, w = 1 + scale).
+ * Statistics are fp32; y is rounded once.
+ *  dtype   SA_BF16 or SA_F32: the type of x and y
+ *  x, y    [rows][cols], row strides ldx, ldy >= cols elements (any, odd ones
+ *          too), aligned to their type; y may be x (then ldy == ldx)
+ *  rows    >= 0 and a multiple of groups (0 launches nothing, and the pointers
+ *          may be NULL); 1 <= cols <= 16384; 1 <= groups <= 65535
+ *  weight, bias  fp32 [groups][cols], or NULL for ones and zeros
+ *  eps     >= 0
+ *  mean, rstd    fp32 [rows] out, or NULL
+ * Rows of whole 16-byte aligned pieces (cols % 8 == 0, x and y 16-byte aligned
+ * with row strides of whole 16 bytes) move 16 bytes a load; others an element.
+ * Errors: SA_ERR_INVALID_ARG; SA_ERR_UNSUPPORTED beyond the limits above. */
+int sparse_attn_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols,
+                           int64_t groups, const float* weight, const float* bias, float eps,
+                           void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Bytes of device workspace of sparse_attn_layer_norm_bwd; 0 for bad sizes. */
+size_t sparse_attn_layer_norm_bwd_workspace_size(int64_t rows, int64_t cols, int64_t groups);
+
+/*
+ * Gradients of sparse_attn_layer_norm: with xh = (x - mean) rstd, g = dy w,
+ *   dx = rstd (g - mean_c(g) - xh mean_c(g xh)),
+ *   dweight = sum dy xh,  dbias = sum dy  over the rows of each group.
+ *  dy, x, dx  of one type, [rows][cols] with row strides of their own; dx may
+ *          be dy or x (with its stride)
+ *  mean, rstd  fp32 [rows], as the forward wrote them
+ *  weight  as in the forward
+ *  dweight, dbias  fp32 [groups][cols] out (written, not added to; zeros for
+ *          rows == 0); each may be NULL
+ *  ws      ws_bytes >= sparse_attn_layer_norm_bwd_workspace_size(); unused
+ *          (may be NULL) when dweight and dbias are NULL
+ * Deterministic: no floating-point atomics.  Limits and errors as above, and
+ * SA_ERR_WORKSPACE. */
+int sparse_attn_layer_norm_bwd(int32_t dtype, const void* dy, int64_t lddy, const void* x,
+                               int64_t ldx, const float* mean, const float* rstd, int64_t rows,
+                               int64_t cols, int64_t groups, const float* weight, void* dx,
+                               int64_t lddx, float* dweight, float* dbias, void* ws,
+                               size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,6 +7,7 @@ fallback: if the shared library is missing, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -23,6 +24,7 @@ __all__ = [
     "sparse_attn_fp8_tiles_bytes", "SA_FP8_K", "SA_FP8_V", "sparse_attn_fwd_fp8", "sparse_attn_comp_state",
     "sparse_attn_comp_out", "SA_OP_COMP_STATE", "COMP_RANK", "make_desc", "EXPORTED_SYMBOLS",
     "sparse_attn_quant_rows_fp8", "sparse_attn_linear_w8a8", "sparse_attn_bwd", "SA_OP_BWD",
+    "sparse_attn_layer_norm", "sparse_attn_layer_norm_bwd", "SA_BF16", "SA_F32",
 ]
 
 # SPARSE_ATTN_LIB names another build of the same library (the CPU sanitizer
@@ -43,6 +45,8 @@ EXPORTED_SYMBOLS = (
     "sparse_attn_quant_fp8_tiles", "sparse_attn_fp8_tiles_bytes", "sparse_attn_fwd_fp8",
     "sparse_attn_comp_state", "sparse_attn_comp_out", "sparse_attn_quant_rows_fp8",
     "sparse_attn_linear_w8a8", "sparse_attn_bwd", "sparse_attn_schedule_static",
+    "sparse_attn_layer_norm", "sparse_attn_layer_norm_bwd_workspace_size",
+    "sparse_attn_layer_norm_bwd",
 )
 
 
@@ -67,6 +71,7 @@ _LIB = None
 _P = ctypes.c_void_p
 _I32P = ctypes.POINTER(ctypes.c_int32)
 _I64P = ctypes.POINTER(ctypes.c_int64)
+_I64 = ctypes.c_int64
 
 
 def library() -> ctypes.CDLL:
@@ -111,6 +116,13 @@ def library() -> ctypes.CDLL:
                                                        ctypes.c_int64, _P, _P, ctypes.c_int64,
                                                        ctypes.c_int64, ctypes.c_int64,
                                                        ctypes.c_int64, _P]),
+            "sparse_attn_layer_norm": (ctypes.c_int, [
+                ctypes.c_int32, _P, _I64, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _I64, _P,
+                _P, _P]),
+            "sparse_attn_layer_norm_bwd_workspace_size": (ctypes.c_size_t, [_I64, _I64, _I64]),
+            "sparse_attn_layer_norm_bwd": (ctypes.c_int, [
+                ctypes.c_int32, _P, _I64, _P, _I64, _P, _P, _I64, _I64, _I64, _P, _P, _I64, _P, _P,
+                _P, ctypes.c_size_t, _P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(lib, name)
@@ -494,3 +506,116 @@ def sparse_attn_bwd(q, k, v, o, d_o, lse, idx, cnt, block: int = 64,
                                    _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream(q))
     _check(st, "sparse_attn_bwd")
     return dq, dk, dv
+
+
+# -------------------------------------------------------------- layer norm
+SA_BF16, SA_F32 = 0, 1
+_NORM_DTYPES = {torch.bfloat16: SA_BF16, torch.float32: SA_F32}
+
+
+def _norm_rows(t, name, dtype=None, shape=None):
+    if t.dim() != 2 or t.dtype not in _NORM_DTYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a 2-D bfloat16 or float32 tensor with unit column stride")
+    if dtype is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {shape}")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _norm_groups(weight, bias, cols, rows):
+    """Groups of rows that the weights [cols] or [groups, cols] speak of."""
+    groups = 1
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is None:
+            continue
+        _dense(t, name, torch.float32)
+        if t.dim() not in (1, 2) or t.shape[-1] != cols:
+            raise ValueError(f"{name} must be [cols] or [groups, cols]")
+        groups = t.shape[0] if t.dim() == 2 else 1
+    if weight is not None and bias is not None and weight.shape != bias.shape:
+        raise ValueError("weight and bias must have one shape")
+    if groups < 1 or rows % groups:
+        raise ValueError("the rows must form equal groups")
+    return groups
+
+
+def _same_device(ref, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name} must be on {ref.device}")
+
+
+def _on(t):
+    """The tensor's device made current for a launch (no work where it is)."""
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        return torch.cuda.device(t.device)
+    return contextlib.nullcontext()
+
+
+def sparse_attn_layer_norm(x, weight=None, bias=None, eps: float = 1e-6, y=None,
+                           with_stats: bool = True):
+    """y = (x - mean) * rstd * weight + bias over the columns of x [rows, cols]
+    (bfloat16 or float32, any row stride).  weight, bias fp32 [cols], or
+    [groups, cols] for equal runs of rows with their own; None: ones, zeros.
+    y may be x.  Returns (y, mean fp32 [rows], rstd fp32 [rows]) (None, None
+    without stats)."""
+    ldx = _norm_rows(x, "x")
+    rows, cols = x.shape
+    groups = _norm_groups(weight, bias, cols, rows)
+    if y is None:
+        y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+    ldy = _norm_rows(y, "y", x.dtype, (rows, cols))
+    _same_device(x, weight=weight, bias=bias, y=y)
+    mean = rstd = None
+    if with_stats:
+        mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device)
+    with _on(x):
+        st = library().sparse_attn_layer_norm(
+            _NORM_DTYPES[x.dtype], _ptr(x), ldx, rows, cols, groups, _ptr(weight), _ptr(bias), eps,
+            _ptr(y), ldy, _ptr(mean), _ptr(rstd), _stream(x))
+    _check(st, "sparse_attn_layer_norm")
+    return y, mean, rstd
+
+
+def sparse_attn_layer_norm_bwd(dy, x, mean, rstd, weight=None, groups: int | None = None,
+                               with_wgrad: bool = True, dx=None, ws=None):
+    """Gradients of sparse_attn_layer_norm for upstream dy: (dx, dweight,
+    dbias), the latter fp32 of weight's shape ([cols] or [groups, cols];
+    without a weight, [groups, cols] if groups is given, else [cols]) or None
+    without wgrad.  mean, rstd are the forward's; dx may be dy."""
+    ldx = _norm_rows(x, "x")
+    rows, cols = x.shape
+    lddy = _norm_rows(dy, "dy", x.dtype, (rows, cols))
+    if weight is not None:
+        have = _norm_groups(weight, None, cols, rows)
+        if groups not in (None, have):
+            raise ValueError("groups and weight disagree")
+        shape, groups = tuple(weight.shape), have
+    else:
+        shape = (cols,) if groups is None else (groups, cols)
+        groups = 1 if groups is None else groups
+        if groups < 1 or rows % groups:
+            raise ValueError("the rows must form equal groups")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _dense(t, name, torch.float32)
+        if tuple(t.shape) != (rows,):
+            raise ValueError(f"{name} must be a [rows] tensor")
+    if dx is None:
+        dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+    lddx = _norm_rows(dx, "dx", x.dtype, (rows, cols))
+    _same_device(x, dy=dy, mean=mean, rstd=rstd, weight=weight, dx=dx, ws=ws)
+    dw = db = None
+    if with_wgrad:
+        dw = torch.empty(shape, dtype=torch.float32, device=x.device)
+        db = torch.empty(shape, dtype=torch.float32, device=x.device)
+        if ws is None:
+            n = library().sparse_attn_layer_norm_bwd_workspace_size(rows, cols, groups)
+            if n == 0:
+                raise SparseAttnError(-2, "workspace size")
+            ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+    with _on(x):
+        st = library().sparse_attn_layer_norm_bwd(
+            _NORM_DTYPES[x.dtype], _ptr(dy), lddy, _ptr(x), ldx, _ptr(mean), _ptr(rstd), rows, cols,
+            groups, _ptr(weight), _ptr(dx), lddx, _ptr(dw), _ptr(db), _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), _stream(x))
+    _check(st, "sparse_attn_layer_norm_bwd")
+    return dx, dw, db

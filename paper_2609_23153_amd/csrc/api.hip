@@ -417,3 +417,92 @@ int sparse_attn_comp_out(const sparse_attn_desc* desc, int32_t rank, const void*
   in.eps = eps;
   return launch_status(sa::launch_comp_out(s, in, static_cast<hipStream_t>(stream)));
 }
+
+// ---- layer norm ------------------------------------------------------------
+namespace {
+// Sizes, strides and element alignment shared by the two calls.
+int check_norm(int32_t dtype, int64_t rows, int64_t cols, int64_t groups) {
+  if (dtype != SA_BF16 && dtype != SA_F32) return SA_ERR_INVALID_ARG;
+  if (rows < 0 || cols < 1 || groups < 1 || rows % groups != 0) return SA_ERR_INVALID_ARG;
+  if (cols > sa::kNormMaxCols || groups > 65535 || rows > ((int64_t)1 << 40))
+    return SA_ERR_UNSUPPORTED;
+  return SA_OK;
+}
+// (without rows nothing is read or written, and the pointers may be null)
+bool norm_tensor_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int32_t dtype) {
+  const uintptr_t elem = dtype == SA_F32 ? 4 : 2;
+  return (p || rows == 0) && reinterpret_cast<uintptr_t>(p) % elem == 0 && ld >= cols &&
+         ld < ((int64_t)1 << 40);
+}
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+}  // namespace
+
+int sparse_attn_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols,
+                           int64_t groups, const float* weight, const float* bias, float eps,
+                           void* y, int64_t ldy, float* mean, float* rstd, void* stream) {
+  const int st = check_norm(dtype, rows, cols, groups);
+  if (st != SA_OK) return st;
+  if (!norm_tensor_ok(x, ldx, rows, cols, dtype) || !norm_tensor_ok(y, ldy, rows, cols, dtype))
+    return SA_ERR_INVALID_ARG;
+  if (!aligned4(weight) || !aligned4(bias) || !aligned4(mean) || !aligned4(rstd))
+    return SA_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || isinf(eps)) return SA_ERR_INVALID_ARG;
+  if (x == y && ldx != ldy) return SA_ERR_INVALID_ARG;
+  sa::LayerNormIn in{};
+  in.x = x;
+  in.weight = weight;
+  in.bias = bias;
+  in.y = y;
+  in.mean = mean;
+  in.rstd = rstd;
+  in.ldx = ldx;
+  in.ldy = ldy;
+  in.rows = rows;
+  in.cols = cols;
+  in.groups = groups;
+  in.eps = eps;
+  in.f32 = dtype == SA_F32;
+  return launch_status(sa::launch_layer_norm(in, static_cast<hipStream_t>(stream)));
+}
+
+size_t sparse_attn_layer_norm_bwd_workspace_size(int64_t rows, int64_t cols, int64_t groups) {
+  if (check_norm(SA_BF16, rows, cols, groups) != SA_OK) return 0;
+  return sa::layer_norm_bwd_workspace_bytes(rows, cols, groups);
+}
+
+int sparse_attn_layer_norm_bwd(int32_t dtype, const void* dy, int64_t lddy, const void* x,
+                               int64_t ldx, const float* mean, const float* rstd, int64_t rows,
+                               int64_t cols, int64_t groups, const float* weight, void* dx,
+                               int64_t lddx, float* dweight, float* dbias, void* ws,
+                               size_t ws_bytes, void* stream) {
+  const int st = check_norm(dtype, rows, cols, groups);
+  if (st != SA_OK) return st;
+  if (!norm_tensor_ok(dy, lddy, rows, cols, dtype) || !norm_tensor_ok(x, ldx, rows, cols, dtype) ||
+      !norm_tensor_ok(dx, lddx, rows, cols, dtype) || (rows > 0 && (!mean || !rstd)))
+    return SA_ERR_INVALID_ARG;
+  if (!aligned4(weight) || !aligned4(mean) || !aligned4(rstd) || !aligned4(dweight) ||
+      !aligned4(dbias) || !aligned4(ws))
+    return SA_ERR_INVALID_ARG;
+  if ((dx == dy && lddx != lddy) || (dx == x && lddx != ldx)) return SA_ERR_INVALID_ARG;
+  if (dweight || dbias) {
+    if (!ws) return SA_ERR_INVALID_ARG;
+    if (ws_bytes < sa::layer_norm_bwd_workspace_bytes(rows, cols, groups)) return SA_ERR_WORKSPACE;
+  }
+  sa::LayerNormBwdIn in{};
+  in.dy = dy;
+  in.x = x;
+  in.mean = mean;
+  in.rstd = rstd;
+  in.weight = weight;
+  in.dx = dx;
+  in.dweight = dweight;
+  in.dbias = dbias;
+  in.lddy = lddy;
+  in.ldx = ldx;
+  in.lddx = lddx;
+  in.rows = rows;
+  in.cols = cols;
+  in.groups = groups;
+  in.f32 = dtype == SA_F32;
+  return launch_status(sa::launch_layer_norm_bwd(in, ws, static_cast<hipStream_t>(stream)));
+}

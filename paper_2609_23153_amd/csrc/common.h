@@ -105,6 +105,24 @@ __device__ __forceinline__ uint32_t wave_sum_u32(uint32_t x) {
   return q[0] + q[1];
 }
 
+// The same for floats.
+__device__ __forceinline__ float wave_sum_f32(float x) {
+#define SA_ROR(n)                                                                              \
+  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + n, \
+                                                             0xF, 0xF, false))
+  SA_ROR(8);
+  SA_ROR(4);
+  SA_ROR(2);
+  SA_ROR(1);
+#undef SA_ROR
+  const uint32_t u = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  const uint32_t v = __float_as_uint(x);
+  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
 // Whole-wave reductions through DPP-free cross-lane shuffles.
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
