@@ -389,6 +389,77 @@ int sparse_attn_linear_w8a8(const uint8_t* xq, const float* sx, int64_t ldx, con
                             const float* sw, int64_t ldw, const float* bias, void* y, int64_t ldy,
                             int64_t M, int64_t N, int64_t K, void* stream);
 
+/*
+ * Paged cache of keys and values for auto-regressive generation (paper §1: the
+ * sparse attention restricted to a causal window).  A page holds 64
+ * consecutive tokens of one sequence: per key head the 8192 e4m3 codes of K
+ * in the SA_FP8_K tile layout of sparse_attn_quant_fp8_tiles, those of V in its
+ * SA_FP8_V layout, and one power-of-two scale each.
+ *  batch       sequences B >= 1
+ *  heads       query heads, a multiple of kv_heads: query head j shares key
+ *              head j / (heads / kv_heads)
+ *  head_dim    must be 128
+ *  tokens      T >= 0 rows of the packed tensors: row q_start[b] + i is the
+ *              i-th new token of sequence b
+ *  num_pages   pages P >= 1 of the pool
+ *  max_pages   entries of a page-table row, 1 <= max_pages < 2^24
+ *  pages_stride  elements from one page-table row to the next (>= max_pages)
+ *  *_stride    element strides of (token, head), channels contiguous
+ *  softmax_scale, causal_chunk, causal_window  as in sparse_attn_desc (the
+ *              position of a token in its sequence decides its chunk)
+ * Device tensors of a cache, contiguous but for the table's rows:
+ *  k8, v8      uint8 [P][kv_heads][8192];  sk, sv  fp32 [P][kv_heads]
+ *  pages       int32 [B][max_pages]: tokens 64 j .. 64 j + 63 of sequence b are
+ *              in page pages[b][j].  Entries outside [0, P) name no page:
+ *              their tokens are not stored and not attended
+ *  q_start     int32 [B + 1], non-decreasing, within [0, T] (kept there)
+ *  kv_len      int32 [B]: tokens of the sequence, its n = q_start[b + 1] -
+ *              q_start[b] new ones (the last n positions) among them
+ * A sequence that has more new tokens than tokens (n > kv_len) breaks the
+ * contract: those at negative positions are not stored, their queries are
+ * not rotated and see no key.
+ */
+typedef struct {
+  int32_t batch, heads, kv_heads, head_dim, tokens, num_pages, max_pages;
+  int64_t pages_stride;
+  int64_t q_stride[2];
+  int64_t k_stride[2];
+  int64_t v_stride[2];
+  int64_t o_stride[2];
+  float softmax_scale;
+  int32_t causal_chunk;
+  int32_t causal_window;
+} sparse_attn_cache_desc;
+
+/*
+ * Appends the packed new tokens' keys and values to the cache.
+ *  k, v     bf16 [T][kv_heads][128] via k_stride, v_stride
+ *  rope     fp32 [rope_rows][rope_dim / 2][2] (cos, sin), or NULL: every key is
+ *           rotated in its first rope_dim channels (a multiple of 8, at most
+ *           128), pairs (2m, 2m+1) as (a c - b s, a s + b c), each fp32
+ *           operation rounded by itself.  A token whose row lies outside the
+ *           table is not rotated
+ *  rope_row int32 [T]: the table's row of every packed token, or NULL: its
+ *           position in its sequence
+ *  q, q_out bf16 [T][heads][128] via q_stride and o_stride, or both NULL: the
+ *           queries, rotated alike (copied without a table) and rounded to
+ *           bf16; q_out may be q (then o_stride == q_stride)
+ * Codes are e4m3(x 2^-e), nearest with ties to even, of the rotated keys and
+ * the values; a page and head has the smallest e >= -126 with amax <= 448 2^e
+ * over the tokens appended to it since its slot 0 was last written, the scale
+ * is 2^e.  When a token raises e, the page's earlier codes are rounded to the
+ * new scale (exact unless they become subnormal).  Slots behind a sequence's
+ * last token keep their codes.  No page may be given to two sequences that get
+ * tokens in it in one call.  Rows of q_out outside every sequence are left
+ * as they are.  T == 0 launches nothing.
+ * Errors: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED (head_dim, sizes beyond 32-bit
+ * work items). */
+int sparse_attn_cache_append(const sparse_attn_cache_desc* desc, const void* k, const void* v,
+                             const float* rope, int64_t rope_rows, int32_t rope_dim,
+                             const int32_t* rope_row, const void* q, void* q_out, uint8_t* k8,
+                             float* sk, uint8_t* v8, float* sv, const int32_t* pages,
+                             const int32_t* q_start, const int32_t* kv_len, void* stream);
+
 /* Element types of the layer-norm calls. */
 enum { SA_BF16 = 0, SA_F32 = 1 };
 

@@ -25,6 +25,7 @@ __all__ = [
     "sparse_attn_comp_out", "SA_OP_COMP_STATE", "COMP_RANK", "make_desc", "EXPORTED_SYMBOLS",
     "sparse_attn_quant_rows_fp8", "sparse_attn_linear_w8a8", "sparse_attn_bwd", "SA_OP_BWD",
     "sparse_attn_layer_norm", "sparse_attn_layer_norm_bwd", "SA_BF16", "SA_F32",
+    "SparseAttnCacheDesc", "sparse_attn_cache_append", "CACHE_PAGE",
 ]
 
 # SPARSE_ATTN_LIB names another build of the same library (the CPU sanitizer
@@ -46,7 +47,7 @@ EXPORTED_SYMBOLS = (
     "sparse_attn_comp_state", "sparse_attn_comp_out", "sparse_attn_quant_rows_fp8",
     "sparse_attn_linear_w8a8", "sparse_attn_bwd", "sparse_attn_schedule_static",
     "sparse_attn_layer_norm", "sparse_attn_layer_norm_bwd_workspace_size",
-    "sparse_attn_layer_norm_bwd",
+    "sparse_attn_layer_norm_bwd", "sparse_attn_cache_append",
 )
 
 
@@ -62,6 +63,18 @@ class SparseAttnDesc(ctypes.Structure):
         ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32),
         ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
         ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3),
+        ("softmax_scale", ctypes.c_float),
+        ("causal_chunk", ctypes.c_int32), ("causal_window", ctypes.c_int32),
+    ]
+
+
+class SparseAttnCacheDesc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("pages_stride", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
+        ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2),
         ("softmax_scale", ctypes.c_float),
         ("causal_chunk", ctypes.c_int32), ("causal_window", ctypes.c_int32),
     ]
@@ -116,6 +129,9 @@ def library() -> ctypes.CDLL:
                                                        ctypes.c_int64, _P, _P, ctypes.c_int64,
                                                        ctypes.c_int64, ctypes.c_int64,
                                                        ctypes.c_int64, _P]),
+            "sparse_attn_cache_append": (ctypes.c_int, [
+                ctypes.POINTER(SparseAttnCacheDesc), _P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P,
+                _P, _P, _P, _P, _P, _P, _P, _P]),
             "sparse_attn_layer_norm": (ctypes.c_int, [
                 ctypes.c_int32, _P, _I64, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _I64, _P,
                 _P, _P]),
@@ -506,6 +522,91 @@ def sparse_attn_bwd(q, k, v, o, d_o, lse, idx, cnt, block: int = 64,
                                    _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream(q))
     _check(st, "sparse_attn_bwd")
     return dq, dk, dv
+
+
+# ------------------------------------------------------- paged e4m3 cache
+CACHE_PAGE = 64                      # tokens of a page
+_CACHE_DESC = struct.Struct("@7i4x9qf2i4x")
+assert _CACHE_DESC.size == ctypes.sizeof(SparseAttnCacheDesc)
+
+
+def _packed(t, name, heads=None, tokens=None):
+    """(token, head) strides of a packed bf16 [T, heads, 128] tensor."""
+    st = t.stride()
+    if t.dim() != 3 or t.dtype != torch.bfloat16 or st[2] != 1 or t.shape[2] != 128:
+        raise ValueError(f"{name} must be a bfloat16 [T, heads, 128] tensor with contiguous channels")
+    if heads is not None and (t.shape[1] != heads or t.shape[0] != tokens):
+        raise ValueError(f"{name} must be [{tokens}, {heads}, 128]")
+    return st[:2]
+
+
+def _cache_pool(k8, sk, v8, sv, pages, q_start, kv_len):
+    """(pages of the pool, key heads, sequences, table entries, table stride)."""
+    for t, name, dt in ((k8, "k8", torch.uint8), (v8, "v8", torch.uint8), (sk, "sk", torch.float32),
+                        (sv, "sv", torch.float32), (q_start, "q_start", torch.int32),
+                        (kv_len, "kv_len", torch.int32)):
+        _dense(t, name, dt)
+    if k8.dim() != 3 or k8.shape[2] != 8192 or v8.shape != k8.shape:
+        raise ValueError("k8 and v8 must be uint8 [pages, kv_heads, 8192]")
+    if sk.shape != k8.shape[:2] or sv.shape != k8.shape[:2]:
+        raise ValueError("sk and sv must be float32 [pages, kv_heads]")
+    if pages.dim() != 2 or pages.dtype != torch.int32 or \
+            (pages.shape[1] > 1 and pages.stride(1) != 1):
+        raise ValueError("pages must be an int32 [batch, max_pages] tensor with contiguous rows")
+    batch, most = pages.shape
+    if tuple(q_start.shape) != (batch + 1,) or tuple(kv_len.shape) != (batch,):
+        raise ValueError("q_start must hold batch + 1 entries and kv_len batch")
+    return k8.shape[0], k8.shape[1], batch, most, max(pages.stride(0), most) if batch == 1 else \
+        pages.stride(0)
+
+
+def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=None,
+                             rope_row=None, q=None, q_out=None):
+    """Appends packed new keys and values, bf16 [T, kv_heads, 128], to a paged
+    cache of e4m3 codes (k8, v8 uint8 [P, kv_heads, 8192], sk, sv fp32 [P,
+    kv_heads], written in place).  pages int32 [B, max_pages] names each
+    sequence's pages of 64 tokens, q_start int32 [B + 1] its packed rows,
+    kv_len int32 [B] its tokens after the call.  rope fp32 [rows, r / 2, 2]
+    rotates the first r channels of the keys, by position or by rope_row int32
+    [T], and of the queries q bf16 [T, heads, 128] if given.  Returns the
+    rotated queries (q_out, which may be q), or None without q."""
+    kst, vst = _packed(k, "k"), _packed(v, "v", k.shape[1], k.shape[0])
+    T, kv, _ = k.shape
+    num, have, batch, most, stride = _cache_pool(k8, sk, v8, sv, pages, q_start, kv_len)
+    if have != kv:
+        raise ValueError("k and k8 must have the same heads")
+    heads, qst, ost = kv, (0, 0), (0, 0)
+    if q is not None:
+        qst = _packed(q, "q")
+        heads = q.shape[1]
+        if q.shape[0] != T or heads % kv:
+            raise ValueError("q must be [T, heads, 128], heads a multiple of the key heads")
+        if q_out is None:
+            q_out = torch.empty(T, heads, 128, dtype=torch.bfloat16, device=q.device)
+        ost = _packed(q_out, "q_out", heads, T)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rows = dim = 0
+    if rope is not None:
+        _dense(rope, "rope", torch.float32)
+        if rope.dim() != 3 or rope.shape[2] != 2:
+            raise ValueError("rope must be float32 [rows, r / 2, 2]")
+        rows, dim = rope.shape[0], 2 * rope.shape[1]
+    if rope_row is not None:
+        _dense(rope_row, "rope_row")
+        if rope is None or tuple(rope_row.shape) != (T,):
+            raise ValueError("rope_row must be an int32 [T] tensor beside rope")
+    _same_device(k, v=v, k8=k8, sk=sk, v8=v8, sv=sv, pages=pages, q_start=q_start, kv_len=kv_len,
+                 rope=rope, rope_row=rope_row, q=q, q_out=q_out)
+    desc = SparseAttnCacheDesc.from_buffer_copy(_CACHE_DESC.pack(
+        batch, heads, kv, 128, T, num, most, stride, *qst, *kst, *vst, *ost, 0.0, 0, 0))
+    with _on(k):
+        st = library().sparse_attn_cache_append(
+            ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(rope), rows, dim, _ptr(rope_row), _ptr(q),
+            _ptr(q_out), _ptr(k8), _ptr(sk), _ptr(v8), _ptr(sv), _ptr(pages), _ptr(q_start),
+            _ptr(kv_len), _stream(k))
+    _check(st, "sparse_attn_cache_append")
+    return q_out
 
 
 # -------------------------------------------------------------- layer norm

@@ -418,6 +418,99 @@ int sparse_attn_comp_out(const sparse_attn_desc* desc, int32_t rank, const void*
   return launch_status(sa::launch_comp_out(s, in, static_cast<hipStream_t>(stream)));
 }
 
+// ---- paged e4m3 cache (paper §1: auto-regressive extension) ----------------
+namespace {
+bool strides2_ok(const int64_t st[2]) {
+  return st[0] >= 0 && (st[0] & 7) == 0 && st[1] >= 0 && (st[1] & 7) == 0;
+}
+
+int check_cache_desc(const sparse_attn_cache_desc* d, sa::CacheIn* c) {
+  if (!d) return SA_ERR_INVALID_ARG;
+  if (d->batch < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
+      d->tokens < 0 || d->num_pages < 1 || d->max_pages < 1 || d->pages_stride < d->max_pages)
+    return SA_ERR_INVALID_ARG;
+  if (!(d->softmax_scale >= 0.f) || isinf(d->softmax_scale)) return SA_ERR_INVALID_ARG;
+  if (d->causal_chunk < 0 || d->causal_window < 0) return SA_ERR_INVALID_ARG;
+  if (d->causal_chunk == 0 && d->causal_window != 0) return SA_ERR_INVALID_ARG;
+  if (d->head_dim != 128) return SA_ERR_UNSUPPORTED;
+  // packed rows and work items are counted in 32 bits, token positions too
+  const int64_t most = (int64_t)1 << 30;
+  if ((int64_t)d->tokens * d->heads > most || (int64_t)d->batch * d->heads > most / 64 ||
+      d->max_pages >= (1 << 24))
+    return SA_ERR_UNSUPPORTED;
+  c->B = d->batch;
+  c->Hkv = d->kv_heads;
+  c->g = d->heads / d->kv_heads;
+  c->T = d->tokens;
+  c->P = d->num_pages;
+  c->max_pages = d->max_pages;
+  c->pages_stride = d->pages_stride;
+  c->chunk = d->causal_chunk;
+  c->window = d->causal_window;
+  return SA_OK;
+}
+
+// The cache's device tensors.
+int check_cache_tensors(sa::CacheIn* c, const uint8_t* k8, const float* sk, const uint8_t* v8,
+                        const float* sv, const int32_t* pages, const int32_t* q_start,
+                        const int32_t* kv_len) {
+  if (!k8 || !sk || !v8 || !sv || !pages || !q_start || !kv_len) return SA_ERR_INVALID_ARG;
+  if (!aligned16(k8) || !aligned16(v8)) return SA_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)sk, (const void*)sv, (const void*)pages, (const void*)q_start,
+                        (const void*)kv_len})
+    if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return SA_ERR_INVALID_ARG;
+  c->k8 = const_cast<uint8_t*>(k8);
+  c->v8 = const_cast<uint8_t*>(v8);
+  c->sk = const_cast<float*>(sk);
+  c->sv = const_cast<float*>(sv);
+  c->pages = pages;
+  c->q_start = q_start;
+  c->kv_len = kv_len;
+  return SA_OK;
+}
+}  // namespace
+
+int sparse_attn_cache_append(const sparse_attn_cache_desc* desc, const void* k, const void* v,
+                             const float* rope, int64_t rope_rows, int32_t rope_dim,
+                             const int32_t* rope_row, const void* q, void* q_out, uint8_t* k8,
+                             float* sk, uint8_t* v8, float* sv, const int32_t* pages,
+                             const int32_t* q_start, const int32_t* kv_len, void* stream) {
+  sa::AppendIn in{};
+  int st = check_cache_desc(desc, &in.c);
+  if (st != SA_OK) return st;
+  if ((st = check_cache_tensors(&in.c, k8, sk, v8, sv, pages, q_start, kv_len)) != SA_OK) return st;
+  if (in.c.T > 0 && (!k || !v)) return SA_ERR_INVALID_ARG;
+  if (in.c.T > 0 && !q != !q_out) return SA_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out)) return SA_ERR_INVALID_ARG;
+  if (!strides2_ok(desc->k_stride) || !strides2_ok(desc->v_stride)) return SA_ERR_INVALID_ARG;
+  if (q && (!strides2_ok(desc->q_stride) || !strides2_ok(desc->o_stride))) return SA_ERR_INVALID_ARG;
+  if (q && q == q_out &&
+      (desc->q_stride[0] != desc->o_stride[0] || desc->q_stride[1] != desc->o_stride[1]))
+    return SA_ERR_INVALID_ARG;
+  if (rope) {
+    if (!aligned16(rope) || rope_rows < 0 || rope_dim < 8 || rope_dim > 128 || (rope_dim & 7) != 0)
+      return SA_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(rope_row) & 3u) != 0) return SA_ERR_INVALID_ARG;
+  }
+  in.k = static_cast<const uint16_t*>(k);
+  in.v = static_cast<const uint16_t*>(v);
+  in.q = static_cast<const uint16_t*>(q);
+  in.q_out = static_cast<uint16_t*>(q_out);
+  in.rope = rope;
+  in.rope_row = rope ? rope_row : nullptr;
+  in.k_tok = desc->k_stride[0];
+  in.k_head = desc->k_stride[1];
+  in.v_tok = desc->v_stride[0];
+  in.v_head = desc->v_stride[1];
+  in.q_tok = desc->q_stride[0];
+  in.q_head = desc->q_stride[1];
+  in.qo_tok = desc->o_stride[0];
+  in.qo_head = desc->o_stride[1];
+  in.rope_rows = rope ? rope_rows : 0;
+  in.rope_dim = rope ? rope_dim : 0;
+  return launch_status(sa::launch_cache_append(in, static_cast<hipStream_t>(stream)));
+}
+
 // ---- layer norm ------------------------------------------------------------
 namespace {
 // Sizes, strides and element alignment shared by the two calls.

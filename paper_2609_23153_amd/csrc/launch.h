@@ -156,6 +156,35 @@ struct LinearIn {
 };
 hipError_t launch_linear_w8a8(const LinearIn& in, hipStream_t stream);
 
+// ---- paged e4m3 cache --------------------------------------------------------
+constexpr int kPage = 64;              // tokens of a page
+constexpr int kPageBytes = 64 * 128;   // codes of a page and head, K or V
+struct CacheIn {
+  uint8_t* k8;             // [P][Hkv][8192], the fp8 forward's K tiles
+  uint8_t* v8;             // [P][Hkv][8192], its V tiles
+  float* sk;               // [P][Hkv] power-of-two scales
+  float* sv;
+  const int32_t* pages;    // [B][max_pages], row stride pages_stride
+  const int32_t* q_start;  // [B + 1] first packed row of every sequence
+  const int32_t* kv_len;   // [B] tokens of every sequence, the new ones among them
+  int64_t pages_stride;
+  int B, Hkv, g, T, P, max_pages;  // g query heads share a key head; T packed rows
+  int chunk, window;               // causal window (chunk 0: none)
+};
+struct AppendIn {
+  CacheIn c;
+  const uint16_t* k;       // bf16 [T][Hkv][128] via strides
+  const uint16_t* v;
+  const uint16_t* q;       // bf16 [T][Hkv g][128] via strides, or null
+  uint16_t* q_out;         // may be q
+  const float* rope;       // fp32 [rope_rows][rope_dim / 2][2], or null
+  const int32_t* rope_row; // [T] rows of the table, or null: positions
+  int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head, qo_tok, qo_head, rope_rows;
+  int rope_dim;
+};
+int64_t cache_append_items(const CacheIn& c);  // (page, sequence) work items at most
+hipError_t launch_cache_append(const AppendIn& in, hipStream_t stream);
+
 // ---- layer norm ------------------------------------------------------------
 constexpr int64_t kNormMaxCols = 16384;  // a row lives in its team's registers
 struct LayerNormIn {

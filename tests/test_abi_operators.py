@@ -84,3 +84,97 @@ def test_layer_norm_bwd_binding_refuses(bad):
     args.update(bad)
     with pytest.raises(ValueError):
         sa.sparse_attn_layer_norm_bwd(**args)
+
+
+# ------------------------------------------------------------- paged cache
+def cache_desc(**kw):
+    d = sa.SparseAttnCacheDesc()
+    f = dict(batch=2, heads=8, kv_heads=4, head_dim=128, tokens=6, num_pages=5, max_pages=3,
+             pages_stride=3, q_stride=(1024, 128), k_stride=(512, 128), v_stride=(512, 128),
+             o_stride=(1024, 128), softmax_scale=0.0, causal_chunk=0, causal_window=0)
+    f.update(kw)
+    for name, value in f.items():
+        if isinstance(value, tuple):
+            getattr(d, name)[:] = value
+        else:
+            setattr(d, name, value)
+    return d
+
+
+BAD_CACHE_DESCS = [
+    (dict(batch=0), INVALID), (dict(heads=6), INVALID), (dict(kv_heads=0), INVALID),
+    (dict(tokens=-1), INVALID), (dict(num_pages=0), INVALID), (dict(max_pages=0), INVALID),
+    (dict(pages_stride=2), INVALID), (dict(head_dim=64), UNSUPPORTED),
+    (dict(causal_chunk=-1), INVALID), (dict(causal_window=3), INVALID),
+    (dict(softmax_scale=-1.0), INVALID), (dict(softmax_scale=float("nan")), INVALID),
+    (dict(max_pages=1 << 24, pages_stride=1 << 24), UNSUPPORTED),
+    (dict(tokens=(1 << 27) + 1), UNSUPPORTED), (dict(batch=1 << 22), UNSUPPORTED),
+]
+
+
+def append(desc=None, k=P, v=P, rope=P, rope_rows=9, rope_dim=128, rope_row=None, q=P, q_out=P,
+           k8=P, sk=P, v8=P, sv=P, pages=P, q_start=P, kv_len=P, **kw):
+    d = cache_desc(**kw)
+    return sa.library().sparse_attn_cache_append(
+        None if desc == "null" else ctypes.byref(d), k, v, rope, rope_rows, rope_dim, rope_row, q,
+        q_out, k8, sk, v8, sv, pages, q_start, kv_len, None)
+
+
+@pytest.mark.parametrize("kw,want", BAD_CACHE_DESCS + [
+    (dict(desc="null"), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID),
+    (dict(k=MIS), INVALID), (dict(v=MIS), INVALID), (dict(q=None), INVALID),
+    (dict(q_out=None), INVALID), (dict(q=MIS), INVALID), (dict(q_out=MIS), INVALID),
+    (dict(q_stride=(1024, 136)), INVALID),           # q_out is q with other strides
+    (dict(q_stride=(1020, 128)), INVALID), (dict(o_stride=(1024, 4)), INVALID),
+    (dict(k_stride=(-512, 128)), INVALID), (dict(v_stride=(512, 129)), INVALID),
+    (dict(rope=MIS), INVALID), (dict(rope_dim=130), INVALID), (dict(rope_dim=12), INVALID),
+    (dict(rope_dim=0), INVALID), (dict(rope_rows=-1), INVALID), (dict(rope_row=ODD), INVALID),
+    (dict(k8=None), INVALID), (dict(v8=MIS), INVALID), (dict(sk=None), INVALID),
+    (dict(sv=ODD), INVALID), (dict(pages=None), INVALID), (dict(pages=MIS), INVALID),
+    (dict(q_start=None), INVALID), (dict(kv_len=None), INVALID),
+])
+def test_cache_append_refuses(kw, want):
+    assert append(**kw) == want
+
+
+def cache_args():
+    """Tensors of a valid append (on the CPU: never launched)."""
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    return dict(k=bf(6, 4, 128), v=bf(6, 4, 128), k8=torch.zeros(5, 4, 8192, dtype=torch.uint8),
+                sk=torch.ones(5, 4), v8=torch.zeros(5, 4, 8192, dtype=torch.uint8),
+                sv=torch.ones(5, 4), pages=i32(2, 3), q_start=i32(3), kv_len=i32(2))
+
+
+BAD_CACHE_TENSORS = [
+    dict(k8=torch.zeros(5, 4, 8192)), dict(k8=torch.zeros(5, 4, 4096, dtype=torch.uint8)),
+    dict(v8=torch.zeros(4, 4, 8192, dtype=torch.uint8)), dict(sk=torch.ones(5, 3)),
+    dict(sv=torch.ones(5, 4, dtype=torch.float64)), dict(pages=torch.zeros(2, 3)),
+    dict(pages=torch.zeros(3, 2, dtype=torch.int32).t()), dict(kv_len=torch.zeros(3, dtype=torch.int32)),
+    dict(q_start=torch.zeros(2, dtype=torch.int32)), dict(kv_len=torch.zeros(2, dtype=torch.int64)),
+]
+
+
+@pytest.mark.parametrize("bad", BAD_CACHE_TENSORS + [
+    dict(k=torch.zeros(6, 4, 128)), dict(k=torch.zeros(6, 4, 64, dtype=torch.bfloat16)),
+    dict(v=torch.zeros(5, 4, 128, dtype=torch.bfloat16)),
+    dict(k=torch.zeros(6, 3, 128, dtype=torch.bfloat16), v=torch.zeros(6, 3, 128, dtype=torch.bfloat16)),
+    dict(q=torch.zeros(6, 6, 128, dtype=torch.bfloat16)),
+    dict(q=torch.zeros(5, 8, 128, dtype=torch.bfloat16)),
+    dict(q_out=torch.zeros(6, 8, 128, dtype=torch.bfloat16)),
+    dict(rope=torch.zeros(9, 64)), dict(rope=torch.zeros(9, 64, 2, dtype=torch.float64)),
+    dict(rope_row=torch.zeros(6, dtype=torch.int32)),
+    dict(rope=torch.zeros(9, 64, 2), rope_row=torch.zeros(5, dtype=torch.int32)),
+    dict(rope=torch.zeros(9, 64, 2), rope_row=torch.zeros(6, dtype=torch.int64)),
+])
+def test_cache_append_binding_refuses(bad):
+    args = cache_args()
+    args.update(bad)
+    with pytest.raises(ValueError):
+        sa.sparse_attn_cache_append(**args)
+
+
+def test_cache_append_binding_reports_the_librarys_refusals():
+    args = cache_args()
+    with pytest.raises(sa.SparseAttnError):               # channels past the head
+        sa.sparse_attn_cache_append(rope=torch.zeros(9, 72, 2), **args)
