@@ -589,8 +589,8 @@ def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=
     rows = dim = 0
     if rope is not None:
         _dense(rope, "rope", torch.float32)
-        if rope.dim() != 3 or rope.shape[2] != 2:
-            raise ValueError("rope must be float32 [rows, r / 2, 2]")
+        if rope.dim() != 3 or rope.shape[2] != 2 or rope.shape[1] % 4 or not 0 < rope.shape[1] <= 64:
+            raise ValueError("rope must be float32 [rows, r / 2, 2], r a multiple of 8 up to 128")
         rows, dim = rope.shape[0], 2 * rope.shape[1]
     if rope_row is not None:
         _dense(rope_row, "rope_row")
