@@ -460,6 +460,35 @@ int sparse_attn_cache_append(const sparse_attn_cache_desc* desc, const void* k, 
                              float* sk, uint8_t* v8, float* sv, const int32_t* pages,
                              const int32_t* q_start, const int32_t* kv_len, void* stream);
 
+/* Bytes of device workspace of sparse_attn_fwd_cache for this descriptor (its
+ * batch, heads, tokens and max_pages count); 0 for an invalid one. */
+size_t sparse_attn_fwd_cache_workspace_size(const sparse_attn_cache_desc* desc);
+
+/*
+ * Exact softmax attention of the packed new tokens over their sequences'
+ * cached tokens.  The query of position t of a sequence of kv_len tokens sees
+ * its keys [0, kv_len), under a causal window those of chunks [c - W + 1, c],
+ * c = t / causal_chunk, among them (chunk 1: token by token), less the tokens
+ * of pages outside the pool:
+ *   o_t = sum_u softmax_u(tau q_t.k_u) v_u,  lse_t = log sum_u exp(tau q_t.k_u)
+ * on the dequantised keys and values; a query that sees no key gets o = 0 and
+ * lse = -inf.  Products accumulate in fp32; the queries enter exactly (but for
+ * 2^-23 of their row's largest element), the probabilities rounded to 8
+ * significant bits, the row sums unrounded.  Cached tokens that some query of
+ * the call sees must be finite; the slots behind the last token may hold
+ * anything.  Call sparse_attn_cache_append for the new tokens first.
+ *  q, o     bf16 [T][heads][128] via q_stride, o_stride; o must not overlap q
+ *  lse      fp32 [T][heads] out, contiguous; may be NULL
+ *  ws       ws_bytes >= sparse_attn_fwd_cache_workspace_size()
+ * Rows of o and lse outside every sequence are left as they are.  T == 0
+ * launches nothing.  Deterministic; a row's last bits depend on how its keys
+ * are cut into parts, which the descriptor's sizes and its own length decide.
+ * Errors: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE. */
+int sparse_attn_fwd_cache(const sparse_attn_cache_desc* desc, const void* q, const uint8_t* k8,
+                          const float* sk, const uint8_t* v8, const float* sv,
+                          const int32_t* pages, const int32_t* q_start, const int32_t* kv_len,
+                          void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Element types of the layer-norm calls. */
 enum { SA_BF16 = 0, SA_F32 = 1 };
 

@@ -26,6 +26,7 @@ __all__ = [
     "sparse_attn_quant_rows_fp8", "sparse_attn_linear_w8a8", "sparse_attn_bwd", "SA_OP_BWD",
     "sparse_attn_layer_norm", "sparse_attn_layer_norm_bwd", "SA_BF16", "SA_F32",
     "SparseAttnCacheDesc", "sparse_attn_cache_append", "CACHE_PAGE",
+    "sparse_attn_fwd_cache",
 ]
 
 # SPARSE_ATTN_LIB names another build of the same library (the CPU sanitizer
@@ -48,6 +49,7 @@ EXPORTED_SYMBOLS = (
     "sparse_attn_linear_w8a8", "sparse_attn_bwd", "sparse_attn_schedule_static",
     "sparse_attn_layer_norm", "sparse_attn_layer_norm_bwd_workspace_size",
     "sparse_attn_layer_norm_bwd", "sparse_attn_cache_append",
+    "sparse_attn_fwd_cache_workspace_size", "sparse_attn_fwd_cache",
 )
 
 
@@ -132,6 +134,11 @@ def library() -> ctypes.CDLL:
             "sparse_attn_cache_append": (ctypes.c_int, [
                 ctypes.POINTER(SparseAttnCacheDesc), _P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P,
                 _P, _P, _P, _P, _P, _P, _P, _P]),
+            "sparse_attn_fwd_cache_workspace_size": (ctypes.c_size_t,
+                                                     [ctypes.POINTER(SparseAttnCacheDesc)]),
+            "sparse_attn_fwd_cache": (ctypes.c_int, [
+                ctypes.POINTER(SparseAttnCacheDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                ctypes.c_size_t, _P]),
             "sparse_attn_layer_norm": (ctypes.c_int, [
                 ctypes.c_int32, _P, _I64, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _I64, _P,
                 _P, _P]),
@@ -607,6 +614,50 @@ def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=
             _ptr(kv_len), _stream(k))
     _check(st, "sparse_attn_cache_append")
     return q_out
+
+
+def sparse_attn_fwd_cache(q, k8, sk, v8, sv, pages, q_start, kv_len, softmax_scale: float = 0.0,
+                          with_lse: bool = True, o=None, lse=None, causal=None, ws=None):
+    """Attention of packed queries, bf16 [T, heads, 128] (row q_start[b] + i:
+    the i-th of the newest tokens of sequence b), over a paged e4m3 cache as
+    sparse_attn_cache_append keeps it.  causal = (chunk_tokens, window_chunks)
+    as for sparse_attn_fwd, by position in the sequence ((1, 0): token by
+    token); None: every query sees its whole sequence.  Returns (o bf16 [T,
+    heads, 128], lse fp32 [T, heads] or None); rows of no sequence are not
+    written."""
+    qst = _packed(q, "q")
+    T, heads, _ = q.shape
+    num, kv, batch, most, stride = _cache_pool(k8, sk, v8, sv, pages, q_start, kv_len)
+    if heads % kv:
+        raise ValueError("the query heads must be a multiple of the key heads")
+    if o is None:
+        o = torch.empty(T, heads, 128, dtype=torch.bfloat16, device=q.device)
+    ost = _packed(o, "o", heads, T)
+    if not with_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.empty(T, heads, dtype=torch.float32, device=q.device)
+    elif tuple(_dense(lse, "lse", torch.float32).shape) != (T, heads):
+        raise ValueError("lse must be [T, heads]")
+    _same_device(q, k8=k8, sk=sk, v8=v8, sv=sv, pages=pages, q_start=q_start, kv_len=kv_len, o=o,
+                 lse=lse, ws=ws)
+    chunk, window = (0, 0) if causal is None else (int(causal[0]), int(causal[1]))
+    desc = SparseAttnCacheDesc.from_buffer_copy(_CACHE_DESC.pack(
+        batch, heads, kv, 128, T, num, most, stride, *qst, 0, 0, 0, 0, *ost, softmax_scale, chunk,
+        window))
+    lib = library()
+    if ws is None:
+        n = lib.sparse_attn_fwd_cache_workspace_size(ctypes.byref(desc))
+        if n == 0:
+            raise SparseAttnError(-2, "workspace size")
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+    with _on(q):
+        st = lib.sparse_attn_fwd_cache(
+            ctypes.byref(desc), _ptr(q), _ptr(k8), _ptr(sk), _ptr(v8), _ptr(sv), _ptr(pages),
+            _ptr(q_start), _ptr(kv_len), _ptr(o), _ptr(lse), _ptr(ws),
+            ws.numel() * ws.element_size(), _stream(q))
+    _check(st, "sparse_attn_fwd_cache")
+    return o, lse
 
 
 # -------------------------------------------------------------- layer norm

@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libsparseattn.so")
 
 SOURCES = ["api.hip", "select.hip", "sched.hip", "fwd_bf16.hip", "fwd_bf16_wave.hip", "fwd_fp8.hip", "quant_fp8.hip",
            "comp.hip", "linear_fp8.hip", "bwd.hip", "layer_norm.hip",
-           "cache_append.hip"]
+           "cache_append.hip", "fwd_cache.hip"]
 # Kernels of one wave per SIMD (512 registers): matrix products write VGPRs,
 # which the vector instructions read directly; the compiler's own choice there
 # is the other half of the register file, with a copy per element.

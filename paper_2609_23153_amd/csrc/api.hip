@@ -511,6 +511,37 @@ int sparse_attn_cache_append(const sparse_attn_cache_desc* desc, const void* k, 
   return launch_status(sa::launch_cache_append(in, static_cast<hipStream_t>(stream)));
 }
 
+size_t sparse_attn_fwd_cache_workspace_size(const sparse_attn_cache_desc* desc) {
+  sa::CacheIn c{};
+  if (check_cache_desc(desc, &c) != SA_OK) return 0;
+  return sa::fwd_cache_workspace_bytes(c);
+}
+
+int sparse_attn_fwd_cache(const sparse_attn_cache_desc* desc, const void* q, const uint8_t* k8,
+                          const float* sk, const uint8_t* v8, const float* sv,
+                          const int32_t* pages, const int32_t* q_start, const int32_t* kv_len,
+                          void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  sa::FwdCacheIn in{};
+  int st = check_cache_desc(desc, &in.c);
+  if (st != SA_OK) return st;
+  if ((st = check_cache_tensors(&in.c, k8, sk, v8, sv, pages, q_start, kv_len)) != SA_OK) return st;
+  if (in.c.T > 0 && (!q || !o || q == o)) return SA_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || !aligned16(q) || !aligned16(o) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u) != 0)
+    return SA_ERR_INVALID_ARG;
+  if (!strides2_ok(desc->q_stride) || !strides2_ok(desc->o_stride)) return SA_ERR_INVALID_ARG;
+  if (ws_bytes < sa::fwd_cache_workspace_bytes(in.c)) return SA_ERR_WORKSPACE;
+  in.q = static_cast<const uint16_t*>(q);
+  in.o = static_cast<uint16_t*>(o);
+  in.lse = lse;
+  in.q_tok = desc->q_stride[0];
+  in.q_head = desc->q_stride[1];
+  in.o_tok = desc->o_stride[0];
+  in.o_head = desc->o_stride[1];
+  in.softmax_scale = desc->softmax_scale > 0.f ? desc->softmax_scale : (float)(1.0 / sqrt(128.0));
+  return launch_status(sa::launch_fwd_cache(in, ws, static_cast<hipStream_t>(stream)));
+}
+
 // ---- layer norm ------------------------------------------------------------
 namespace {
 // Sizes, strides and element alignment shared by the two calls.

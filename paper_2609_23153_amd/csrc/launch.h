@@ -185,6 +185,18 @@ struct AppendIn {
 int64_t cache_append_items(const CacheIn& c);  // (page, sequence) work items at most
 hipError_t launch_cache_append(const AppendIn& in, hipStream_t stream);
 
+struct FwdCacheIn {
+  CacheIn c;
+  const uint16_t* q;       // bf16 [T][Hkv g][128] via strides
+  uint16_t* o;             // bf16, likewise
+  float* lse;              // [T][Hkv g] or null
+  int64_t q_tok, q_head, o_tok, o_head;
+  float softmax_scale;
+};
+// Workspace: the parts' shares, fp32 [parts][T Hkv g][128] and (max, sum) pairs.
+size_t fwd_cache_workspace_bytes(const CacheIn& c);
+hipError_t launch_fwd_cache(const FwdCacheIn& in, void* ws, hipStream_t stream);
+
 // ---- layer norm ------------------------------------------------------------
 constexpr int64_t kNormMaxCols = 16384;  // a row lives in its team's registers
 struct LayerNormIn {

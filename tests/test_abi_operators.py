@@ -173,3 +173,49 @@ def test_cache_append_binding_refuses(bad):
     args.update(bad)
     with pytest.raises(ValueError):
         sa.sparse_attn_cache_append(**args)
+
+
+def fwd_cache(desc=None, q=P, k8=P, sk=P, v8=P, sv=P, pages=P, q_start=P, kv_len=P,
+              o=ctypes.c_void_p(1 << 21), lse=P, ws=P, ws_bytes=WS, **kw):
+    d = cache_desc(**kw)
+    return sa.library().sparse_attn_fwd_cache(
+        None if desc == "null" else ctypes.byref(d), q, k8, sk, v8, sv, pages, q_start, kv_len, o,
+        lse, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,want", BAD_CACHE_DESCS + [
+    (dict(desc="null"), INVALID), (dict(q=None), INVALID), (dict(o=None), INVALID),
+    (dict(o=P), INVALID),                            # o is q
+    (dict(q=MIS), INVALID), (dict(o=MIS), INVALID), (dict(lse=MIS), INVALID),
+    (dict(ws=None), INVALID), (dict(ws=MIS), INVALID), (dict(ws_bytes=8), WORKSPACE),
+    (dict(q_stride=(1024, 12)), INVALID), (dict(o_stride=(-8, 128)), INVALID),
+    (dict(k8=MIS), INVALID), (dict(v8=None), INVALID), (dict(sk=ODD), INVALID),
+    (dict(sv=None), INVALID), (dict(pages=None), INVALID), (dict(q_start=MIS), INVALID),
+    (dict(kv_len=None), INVALID),
+])
+def test_fwd_cache_refuses(kw, want):
+    assert fwd_cache(**kw) == want
+
+
+def test_fwd_cache_workspace():
+    size = lambda **kw: sa.library().sparse_attn_fwd_cache_workspace_size(ctypes.byref(cache_desc(**kw)))
+    assert size(heads=6) == 0 and size(head_dim=64) == 0
+    assert sa.library().sparse_attn_fwd_cache_workspace_size(None) == 0
+    assert size() >= 16 and size(tokens=0) >= 16
+    # parts are bounded: one long sequence, 64 of them
+    one = size(batch=1, tokens=1, max_pages=1 << 20, pages_stride=1 << 20)
+    assert one == 64 * 8 * (128 * 4 + 8)
+
+
+@pytest.mark.parametrize("bad", BAD_CACHE_TENSORS + [
+    dict(q=torch.zeros(6, 8, 128)), dict(q=torch.zeros(6, 6, 128, dtype=torch.bfloat16)),
+    dict(o=torch.zeros(5, 8, 128, dtype=torch.bfloat16)), dict(o=torch.zeros(6, 8, 128)),
+    dict(lse=torch.zeros(8, 6)), dict(lse=torch.zeros(6, 8, dtype=torch.float64)),
+])
+def test_fwd_cache_binding_refuses(bad):
+    args = cache_args()
+    del args["k"], args["v"]
+    args["q"] = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    args.update(bad)
+    with pytest.raises(ValueError):
+        sa.sparse_attn_fwd_cache(**args)
