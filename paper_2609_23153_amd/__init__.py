@@ -7,7 +7,6 @@ fallback: if the shared library is missing, every call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -132,12 +131,11 @@ def library() -> ctypes.CDLL:
                                                        ctypes.c_int64, ctypes.c_int64,
                                                        ctypes.c_int64, _P]),
             "sparse_attn_cache_append": (ctypes.c_int, [
-                ctypes.POINTER(SparseAttnCacheDesc), _P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P,
+                _P, _P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P,
                 _P, _P, _P, _P, _P, _P, _P, _P]),
-            "sparse_attn_fwd_cache_workspace_size": (ctypes.c_size_t,
-                                                     [ctypes.POINTER(SparseAttnCacheDesc)]),
+            "sparse_attn_fwd_cache_workspace_size": (ctypes.c_size_t, [_P]),
             "sparse_attn_fwd_cache": (ctypes.c_int, [
-                ctypes.POINTER(SparseAttnCacheDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                 ctypes.c_size_t, _P]),
             "sparse_attn_layer_norm": (ctypes.c_int, [
                 ctypes.c_int32, _P, _I64, _I64, _I64, _I64, _P, _P, ctypes.c_float, _P, _I64, _P,
@@ -531,40 +529,57 @@ def sparse_attn_bwd(q, k, v, o, d_o, lse, idx, cnt, block: int = 64,
     return dq, dk, dv
 
 
+# The calls below are made once a token or a layer, where the time of the
+# checks counts: every tensor is looked at once.
+def _arr(t, name, dtype, dev, numel):
+    """Device address of a dense tensor of `numel` elements."""
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != dev or \
+            not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {numel} elements beside "
+                         "the others")
+    return t.data_ptr()
+
+
+def _elsewhere(dev):
+    """Whether the tensors' device is not the current one (the call is then
+    repeated with it current)."""
+    return dev >= 0 and dev != torch._C._cuda_getDevice()
+
+
 # ------------------------------------------------------- paged e4m3 cache
 CACHE_PAGE = 64                      # tokens of a page
 _CACHE_DESC = struct.Struct("@7i4x9qf2i4x")
 assert _CACHE_DESC.size == ctypes.sizeof(SparseAttnCacheDesc)
 
 
-def _packed(t, name, heads=None, tokens=None):
-    """(token, head) strides of a packed bf16 [T, heads, 128] tensor."""
+def _packed(t, name, dev, heads, tokens):
+    """(token, head) strides of a packed bf16 [tokens, heads, 128] tensor."""
     st = t.stride()
-    if t.dim() != 3 or t.dtype != torch.bfloat16 or st[2] != 1 or t.shape[2] != 128:
-        raise ValueError(f"{name} must be a bfloat16 [T, heads, 128] tensor with contiguous channels")
-    if heads is not None and (t.shape[1] != heads or t.shape[0] != tokens):
-        raise ValueError(f"{name} must be [{tokens}, {heads}, 128]")
-    return st[:2]
+    if t.dtype is not torch.bfloat16 or t.shape != (tokens, heads, 128) or st[2] != 1 or \
+            t.get_device() != dev:
+        raise ValueError(f"{name} must be a bfloat16 [{tokens}, {heads}, 128] tensor with "
+                         "contiguous channels beside the others")
+    return st[0] if tokens > 1 else 0, st[1] if heads > 1 else 0
 
 
-def _cache_pool(k8, sk, v8, sv, pages, q_start, kv_len):
-    """(pages of the pool, key heads, sequences, table entries, table stride)."""
-    for t, name, dt in ((k8, "k8", torch.uint8), (v8, "v8", torch.uint8), (sk, "sk", torch.float32),
-                        (sv, "sv", torch.float32), (q_start, "q_start", torch.int32),
-                        (kv_len, "kv_len", torch.int32)):
-        _dense(t, name, dt)
-    if k8.dim() != 3 or k8.shape[2] != 8192 or v8.shape != k8.shape:
+def _cache_pool(dev, k8, sk, v8, sv, pages, q_start, kv_len):
+    """(pages of the pool, key heads, sequences, table entries, table stride)
+    and the tensors' addresses."""
+    shape = k8.shape
+    if len(shape) != 3 or shape[2] != 8192:
         raise ValueError("k8 and v8 must be uint8 [pages, kv_heads, 8192]")
-    if sk.shape != k8.shape[:2] or sv.shape != k8.shape[:2]:
-        raise ValueError("sk and sv must be float32 [pages, kv_heads]")
-    if pages.dim() != 2 or pages.dtype != torch.int32 or \
-            (pages.shape[1] > 1 and pages.stride(1) != 1):
-        raise ValueError("pages must be an int32 [batch, max_pages] tensor with contiguous rows")
-    batch, most = pages.shape
-    if tuple(q_start.shape) != (batch + 1,) or tuple(kv_len.shape) != (batch,):
-        raise ValueError("q_start must hold batch + 1 entries and kv_len batch")
-    return k8.shape[0], k8.shape[1], batch, most, max(pages.stride(0), most) if batch == 1 else \
-        pages.stride(0)
+    num, kv, _ = shape
+    if pages.dim() != 2 or pages.dtype is not torch.int32 or pages.get_device() != dev:
+        raise ValueError("pages must be an int32 [batch, max_pages] tensor beside the others")
+    (batch, most), (stride, unit) = pages.shape, pages.stride()
+    if unit != 1 and most > 1:
+        raise ValueError("the rows of pages must be contiguous")
+    n = num * kv
+    return (num, kv, batch, most, stride if batch > 1 else most), (
+        _arr(k8, "k8", torch.uint8, dev, n * 8192), _arr(sk, "sk", torch.float32, dev, n),
+        _arr(v8, "v8", torch.uint8, dev, n * 8192), _arr(sv, "sv", torch.float32, dev, n),
+        pages.data_ptr(), _arr(q_start, "q_start", torch.int32, dev, batch + 1),
+        _arr(kv_len, "kv_len", torch.int32, dev, batch))
 
 
 def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=None,
@@ -577,41 +592,42 @@ def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=
     rotates the first r channels of the keys, by position or by rope_row int32
     [T], and of the queries q bf16 [T, heads, 128] if given.  Returns the
     rotated queries (q_out, which may be q), or None without q."""
-    kst, vst = _packed(k, "k"), _packed(v, "v", k.shape[1], k.shape[0])
-    T, kv, _ = k.shape
-    num, have, batch, most, stride = _cache_pool(k8, sk, v8, sv, pages, q_start, kv_len)
-    if have != kv:
-        raise ValueError("k and k8 must have the same heads")
-    heads, qst, ost = kv, (0, 0), (0, 0)
+    dev = k.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope,
+                                            rope_row, q, q_out)
+    (num, kv, batch, most, stride), cache = _cache_pool(dev, k8, sk, v8, sv, pages, q_start, kv_len)
+    T = k.shape[0]
+    k0, k1 = _packed(k, "k", dev, kv, T)
+    v0, v1 = _packed(v, "v", dev, kv, T)
+    heads, q0, q1, o0, o1, qp, op = kv, 0, 0, 0, 0, None, None
     if q is not None:
-        qst = _packed(q, "q")
-        heads = q.shape[1]
-        if q.shape[0] != T or heads % kv:
+        if q.dim() != 3 or q.shape[1] % kv:
             raise ValueError("q must be [T, heads, 128], heads a multiple of the key heads")
+        heads = q.shape[1]
+        q0, q1 = _packed(q, "q", dev, heads, T)
         if q_out is None:
-            q_out = torch.empty(T, heads, 128, dtype=torch.bfloat16, device=q.device)
-        ost = _packed(q_out, "q_out", heads, T)
+            q_out = torch.empty_like(q)
+        o0, o1 = (q0, q1) if q_out is q else _packed(q_out, "q_out", dev, heads, T)
+        qp, op = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
     rows = dim = 0
+    cs = row = None
     if rope is not None:
-        _dense(rope, "rope", torch.float32)
         if rope.dim() != 3 or rope.shape[2] != 2 or rope.shape[1] % 4 or not 0 < rope.shape[1] <= 64:
             raise ValueError("rope must be float32 [rows, r / 2, 2], r a multiple of 8 up to 128")
         rows, dim = rope.shape[0], 2 * rope.shape[1]
+        cs = _arr(rope, "rope", torch.float32, dev, rows * dim)
     if rope_row is not None:
-        _dense(rope_row, "rope_row")
-        if rope is None or tuple(rope_row.shape) != (T,):
-            raise ValueError("rope_row must be an int32 [T] tensor beside rope")
-    _same_device(k, v=v, k8=k8, sk=sk, v8=v8, sv=sv, pages=pages, q_start=q_start, kv_len=kv_len,
-                 rope=rope, rope_row=rope_row, q=q, q_out=q_out)
-    desc = SparseAttnCacheDesc.from_buffer_copy(_CACHE_DESC.pack(
-        batch, heads, kv, 128, T, num, most, stride, *qst, *kst, *vst, *ost, 0.0, 0, 0))
-    with _on(k):
-        st = library().sparse_attn_cache_append(
-            ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(rope), rows, dim, _ptr(rope_row), _ptr(q),
-            _ptr(q_out), _ptr(k8), _ptr(sk), _ptr(v8), _ptr(sv), _ptr(pages), _ptr(q_start),
-            _ptr(kv_len), _stream(k))
+        if rope is None:
+            raise ValueError("rope_row without rope")
+        row = _arr(rope_row, "rope_row", torch.int32, dev, T)
+    desc = _CACHE_DESC.pack(batch, heads, kv, 128, T, num, most, stride, q0, q1, k0, k1, v0, v1, o0,
+                            o1, 0.0, 0, 0)
+    st = library().sparse_attn_cache_append(desc, k.data_ptr(), v.data_ptr(), cs, rows, dim, row, qp,
+                                            op, *cache, _stream(k))
     _check(st, "sparse_attn_cache_append")
     return q_out
 
@@ -625,37 +641,43 @@ def sparse_attn_fwd_cache(q, k8, sk, v8, sv, pages, q_start, kv_len, softmax_sca
     token); None: every query sees its whole sequence.  Returns (o bf16 [T,
     heads, 128], lse fp32 [T, heads] or None); rows of no sequence are not
     written."""
-    qst = _packed(q, "q")
+    dev = q.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sparse_attn_fwd_cache(q, k8, sk, v8, sv, pages, q_start, kv_len, softmax_scale,
+                                         with_lse, o, lse, causal, ws)
+    (num, kv, batch, most, stride), cache = _cache_pool(dev, k8, sk, v8, sv, pages, q_start, kv_len)
+    if q.dim() != 3 or q.shape[1] % kv:
+        raise ValueError("q must be [T, heads, 128], heads a multiple of the key heads")
     T, heads, _ = q.shape
-    num, kv, batch, most, stride = _cache_pool(k8, sk, v8, sv, pages, q_start, kv_len)
-    if heads % kv:
-        raise ValueError("the query heads must be a multiple of the key heads")
+    q0, q1 = _packed(q, "q", dev, heads, T)
     if o is None:
-        o = torch.empty(T, heads, 128, dtype=torch.bfloat16, device=q.device)
-    ost = _packed(o, "o", heads, T)
+        o = torch.empty_like(q)
+    o0, o1 = _packed(o, "o", dev, heads, T)
+    lp = None
     if not with_lse:
         lse = None
     elif lse is None:
-        lse = torch.empty(T, heads, dtype=torch.float32, device=q.device)
-    elif tuple(_dense(lse, "lse", torch.float32).shape) != (T, heads):
-        raise ValueError("lse must be [T, heads]")
-    _same_device(q, k8=k8, sk=sk, v8=v8, sv=sv, pages=pages, q_start=q_start, kv_len=kv_len, o=o,
-                 lse=lse, ws=ws)
-    chunk, window = (0, 0) if causal is None else (int(causal[0]), int(causal[1]))
-    desc = SparseAttnCacheDesc.from_buffer_copy(_CACHE_DESC.pack(
-        batch, heads, kv, 128, T, num, most, stride, *qst, 0, 0, 0, 0, *ost, softmax_scale, chunk,
-        window))
+        lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
+        lp = lse.data_ptr()
+    else:
+        lp = _arr(lse, "lse", torch.float32, dev, T * heads)
+        if lse.shape != (T, heads):
+            raise ValueError("lse must be [T, heads]")
+    chunk, window = (0, 0) if causal is None else causal
+    desc = _CACHE_DESC.pack(batch, heads, kv, 128, T, num, most, stride, q0, q1, 0, 0, 0, 0, o0, o1,
+                            softmax_scale, int(chunk), int(window))
     lib = library()
     if ws is None:
-        n = lib.sparse_attn_fwd_cache_workspace_size(ctypes.byref(desc))
+        n = lib.sparse_attn_fwd_cache_workspace_size(desc)
         if n == 0:
             raise SparseAttnError(-2, "workspace size")
         ws = torch.empty(n, dtype=torch.uint8, device=q.device)
-    with _on(q):
-        st = lib.sparse_attn_fwd_cache(
-            ctypes.byref(desc), _ptr(q), _ptr(k8), _ptr(sk), _ptr(v8), _ptr(sv), _ptr(pages),
-            _ptr(q_start), _ptr(kv_len), _ptr(o), _ptr(lse), _ptr(ws),
-            ws.numel() * ws.element_size(), _stream(q))
+    else:
+        n = ws.numel() * ws.element_size()
+        _arr(ws, "ws", ws.dtype, dev, ws.numel())
+    st = lib.sparse_attn_fwd_cache(desc, q.data_ptr(), *cache, o.data_ptr(), lp, ws.data_ptr(), n,
+                                   _stream(q))
     _check(st, "sparse_attn_fwd_cache")
     return o, lse
 
@@ -665,42 +687,31 @@ SA_BF16, SA_F32 = 0, 1
 _NORM_DTYPES = {torch.bfloat16: SA_BF16, torch.float32: SA_F32}
 
 
-def _norm_rows(t, name, dtype=None, shape=None):
-    if t.dim() != 2 or t.dtype not in _NORM_DTYPES or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a 2-D bfloat16 or float32 tensor with unit column stride")
-    if dtype is not None and (t.dtype != dtype or tuple(t.shape) != shape):
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {shape}")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+def _norm_rows(t, name, dtype, shape, dev):
+    """Row stride of a [rows, cols] tensor with unit column stride."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or (st[1] != 1 and shape[1] > 1) or \
+            t.get_device() != dev:
+        raise ValueError(f"{name} must be a {dtype} {tuple(shape)} tensor with unit column stride "
+                         "beside the others")
+    return st[0] if shape[0] > 1 else shape[1]
 
 
-def _norm_groups(weight, bias, cols, rows):
-    """Groups of rows that the weights [cols] or [groups, cols] speak of."""
-    groups = 1
-    for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is None:
-            continue
-        _dense(t, name, torch.float32)
-        if t.dim() not in (1, 2) or t.shape[-1] != cols:
-            raise ValueError(f"{name} must be [cols] or [groups, cols]")
-        groups = t.shape[0] if t.dim() == 2 else 1
-    if weight is not None and bias is not None and weight.shape != bias.shape:
-        raise ValueError("weight and bias must have one shape")
-    if groups < 1 or rows % groups:
-        raise ValueError("the rows must form equal groups")
-    return groups
+def _norm_input(x):
+    """(type code, rows, cols) of an input."""
+    code = _NORM_DTYPES.get(x.dtype)
+    if code is None or x.dim() != 2:
+        raise ValueError("x must be a 2-D bfloat16 or float32 tensor")
+    return code, *x.shape
 
 
-def _same_device(ref, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"{name} must be on {ref.device}")
-
-
-def _on(t):
-    """The tensor's device made current for a launch (no work where it is)."""
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        return torch.cuda.device(t.device)
-    return contextlib.nullcontext()
+def _norm_weight(t, name, rows, cols, dev):
+    """Address and groups of a weight [cols] or [groups, cols]."""
+    shape = t.shape
+    groups = shape[0] if len(shape) == 2 else 1
+    if len(shape) not in (1, 2) or shape[-1] != cols or groups < 1 or rows % groups:
+        raise ValueError(f"{name} must be [cols] or [groups, cols], the rows in equal groups")
+    return _arr(t, name, torch.float32, dev, groups * cols), groups
 
 
 def sparse_attn_layer_norm(x, weight=None, bias=None, eps: float = 1e-6, y=None,
@@ -710,20 +721,32 @@ def sparse_attn_layer_norm(x, weight=None, bias=None, eps: float = 1e-6, y=None,
     [groups, cols] for equal runs of rows with their own; None: ones, zeros.
     y may be x.  Returns (y, mean fp32 [rows], rstd fp32 [rows]) (None, None
     without stats)."""
-    ldx = _norm_rows(x, "x")
-    rows, cols = x.shape
-    groups = _norm_groups(weight, bias, cols, rows)
+    dev = x.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sparse_attn_layer_norm(x, weight, bias, eps, y, with_stats)
+    code, rows, cols = _norm_input(x)
+    ldx = _norm_rows(x, "x", x.dtype, x.shape, dev)
+    groups, wp, bp = 1, None, None
+    if weight is not None:
+        wp, groups = _norm_weight(weight, "weight", rows, cols, dev)
+    if bias is not None:
+        bp, n = _norm_weight(bias, "bias", rows, cols, dev)
+        if weight is not None and n != groups:
+            raise ValueError("weight and bias must have the same groups")
+        groups = n
     if y is None:
-        y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-    ldy = _norm_rows(y, "y", x.dtype, (rows, cols))
-    _same_device(x, weight=weight, bias=bias, y=y)
-    mean = rstd = None
+        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        ldy = cols
+    else:
+        ldy = _norm_rows(y, "y", x.dtype, x.shape, dev)
+    mean = rstd = mp = rp = None
     if with_stats:
-        mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device)
-    with _on(x):
-        st = library().sparse_attn_layer_norm(
-            _NORM_DTYPES[x.dtype], _ptr(x), ldx, rows, cols, groups, _ptr(weight), _ptr(bias), eps,
-            _ptr(y), ldy, _ptr(mean), _ptr(rstd), _stream(x))
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+        mp, rp = mean.data_ptr(), rstd.data_ptr()
+    st = library().sparse_attn_layer_norm(code, x.data_ptr(), ldx, rows, cols, groups, wp, bp, eps,
+                                          y.data_ptr(), ldy, mp, rp, _stream(x))
     _check(st, "sparse_attn_layer_norm")
     return y, mean, rstd
 
@@ -734,40 +757,49 @@ def sparse_attn_layer_norm_bwd(dy, x, mean, rstd, weight=None, groups: int | Non
     dbias), the latter fp32 of weight's shape ([cols] or [groups, cols];
     without a weight, [groups, cols] if groups is given, else [cols]) or None
     without wgrad.  mean, rstd are the forward's; dx may be dy."""
-    ldx = _norm_rows(x, "x")
-    rows, cols = x.shape
-    lddy = _norm_rows(dy, "dy", x.dtype, (rows, cols))
+    dev = x.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sparse_attn_layer_norm_bwd(dy, x, mean, rstd, weight, groups, with_wgrad, dx, ws)
+    code, rows, cols = _norm_input(x)
+    ldx = _norm_rows(x, "x", x.dtype, x.shape, dev)
+    lddy = _norm_rows(dy, "dy", x.dtype, x.shape, dev)
+    wp = None
     if weight is not None:
-        have = _norm_groups(weight, None, cols, rows)
+        wp, have = _norm_weight(weight, "weight", rows, cols, dev)
         if groups not in (None, have):
             raise ValueError("groups and weight disagree")
-        shape, groups = tuple(weight.shape), have
+        shape, groups = weight.shape, have
     else:
         shape = (cols,) if groups is None else (groups, cols)
         groups = 1 if groups is None else groups
         if groups < 1 or rows % groups:
             raise ValueError("the rows must form equal groups")
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _dense(t, name, torch.float32)
-        if tuple(t.shape) != (rows,):
-            raise ValueError(f"{name} must be a [rows] tensor")
+    mp = _arr(mean, "mean", torch.float32, dev, rows)
+    rp = _arr(rstd, "rstd", torch.float32, dev, rows)
     if dx is None:
-        dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-    lddx = _norm_rows(dx, "dx", x.dtype, (rows, cols))
-    _same_device(x, dy=dy, mean=mean, rstd=rstd, weight=weight, dx=dx, ws=ws)
-    dw = db = None
+        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        lddx = cols
+    else:
+        lddx = _norm_rows(dx, "dx", x.dtype, x.shape, dev)
+    lib = library()
+    dw = db = dwp = dbp = wsp = None
+    n = 0
     if with_wgrad:
         dw = torch.empty(shape, dtype=torch.float32, device=x.device)
-        db = torch.empty(shape, dtype=torch.float32, device=x.device)
+        db = torch.empty_like(dw)
+        dwp, dbp = dw.data_ptr(), db.data_ptr()
         if ws is None:
-            n = library().sparse_attn_layer_norm_bwd_workspace_size(rows, cols, groups)
+            n = lib.sparse_attn_layer_norm_bwd_workspace_size(rows, cols, groups)
             if n == 0:
                 raise SparseAttnError(-2, "workspace size")
             ws = torch.empty(n, dtype=torch.uint8, device=x.device)
-    with _on(x):
-        st = library().sparse_attn_layer_norm_bwd(
-            _NORM_DTYPES[x.dtype], _ptr(dy), lddy, _ptr(x), ldx, _ptr(mean), _ptr(rstd), rows, cols,
-            groups, _ptr(weight), _ptr(dx), lddx, _ptr(dw), _ptr(db), _ptr(ws),
-            0 if ws is None else ws.numel() * ws.element_size(), _stream(x))
+        else:
+            n = ws.numel() * ws.element_size()
+            _arr(ws, "ws", ws.dtype, dev, ws.numel())
+        wsp = ws.data_ptr()
+    st = lib.sparse_attn_layer_norm_bwd(code, dy.data_ptr(), lddy, x.data_ptr(), ldx, mp, rp, rows,
+                                        cols, groups, wp, dx.data_ptr(), lddx, dwp, dbp, wsp, n,
+                                        _stream(x))
     _check(st, "sparse_attn_layer_norm_bwd")
     return dx, dw, db
