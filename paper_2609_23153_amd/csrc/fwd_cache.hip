@@ -18,15 +18,12 @@
 //              page through LDS, copied two pages ahead
 // Long key ranges are cut over workgroups when there are few rows: partial
 // sums go to the workspace and a second kernel joins them in a fixed order.
+#include <type_traits>
+
 #include "cache.h"
 
 namespace sa {
 namespace {
-
-// Read-only here: reads through the constant address space are scalar loads,
-// which do not wait for vector loads and copies in flight.
-typedef const __attribute__((address_space(4))) int32_t* table_ptr;
-typedef const __attribute__((address_space(4))) float* scale_ptr;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
@@ -104,18 +101,17 @@ struct Wave {
   bool valid;
 };
 
-__device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d) {
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+// e4m3 codes of four values.  (Both halves of the word are written: what it
+// holds before does not matter.)
+__device__ __forceinline__ int cvt4(float a, float b, float c, float d) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, __builtin_nondeterministic_value(0), false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
-// e4m3 terms of four values: h = e4m3(x), l = e4m3((x - h) 2^rest).
-__device__ __forceinline__ void split4(const float (&x)[4], float up, int* h, int* l) {
-  const uint32_t w = cvt4(x[0], x[1], x[2], x[3]);
-  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)w, up, false);
-  const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)w, up, true);
-  *h = (int)w;
-  *l = (int)cvt4(fmaf(x[0], up, -a[0]), fmaf(x[1], up, -a[1]), fmaf(x[2], up, -b[0]),
-                 fmaf(x[3], up, -b[1]));
+// The rests (x - h) up of four values whose codes h holds, as codes.
+__device__ __forceinline__ int rest4(float x0, float x1, float x2, float x3, int h, float up) {
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, up, false);
+  const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, up, true);
+  return cvt4(fmaf(x0, up, -a[0]), fmaf(x1, up, -a[1]), fmaf(x2, up, -b[0]), fmaf(x3, up, -b[1]));
 }
 
 __device__ __forceinline__ float pair_sum32(float x) {
@@ -164,10 +160,9 @@ __device__ __forceinline__ void wave_init(const Params& p, const Tile& t, int h,
     for (int j = 0; j < 8; ++j) {
       const uint32_t a = x[ks][j / 2][2 * (j & 1)], b = x[ks][j / 2][2 * (j & 1) + 1];
       const float v[4] = {bf16_lo(a) * inv, bf16_hi(a) * inv, bf16_lo(b) * inv, bf16_hi(b) * inv};
-      int hi, lo;
-      split4(v, (float)(1 << kRestQ), &hi, &lo);
+      const int hi = cvt4(v[0], v[1], v[2], v[3]);
       w->qh[ks][j] = hi;
-      w->ql[ks][j] = lo;
+      w->ql[ks][j] = rest4(v[0], v[1], v[2], v[3], hi, (float)(1 << kRestQ));
     }
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -180,15 +175,12 @@ __device__ __forceinline__ void wave_init(const Params& p, const Tile& t, int h,
 #define SA_MFMA(a, b, c, ca, cb) \
   __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, ca, 0, cb)
 
-// S^T (64 keys x 32 rows) of a page: K fragments kf[2 rt + ks].
-__device__ __forceinline__ void scores(const Wave& w, const i32x8 (&kf)[4], int sk, f32x16 (&s)[2]) {
-#pragma unroll
-  for (int rt = 0; rt < 2; ++rt) {
-    s[rt] = SA_MFMA(kf[2 * rt], w.ql[0], (f32x16){}, sk, w.ql_code);
-    s[rt] = SA_MFMA(kf[2 * rt + 1], w.ql[1], s[rt], sk, w.ql_code);
-    s[rt] = SA_MFMA(kf[2 * rt], w.qh[0], s[rt], sk, w.qh_code);
-    s[rt] = SA_MFMA(kf[2 * rt + 1], w.qh[1], s[rt], sk, w.qh_code);
-  }
+// S^T of 32 keys of a page x 32 rows: K fragments k0, k1 (channels 0-63, 64-127).
+__device__ __forceinline__ f32x16 scores(const Wave& w, const i32x8& k0, const i32x8& k1, int sk) {
+  f32x16 s = SA_MFMA(k0, w.ql[0], (f32x16){}, sk, w.ql_code);
+  s = SA_MFMA(k1, w.ql[1], s, sk, w.ql_code);
+  s = SA_MFMA(k0, w.qh[0], s, sk, w.qh_code);
+  return SA_MFMA(k1, w.qh[1], s, sk, w.qh_code);
 }
 
 // Scores of keys outside a row's range (page's first key: start) become -inf.
@@ -204,16 +196,19 @@ __device__ __forceinline__ void mask_scores(const Wave& w, int start, f32x16 (&s
     }
 }
 
-// Softmax numerators of a page as two e4m3 terms, slot 16 rt + r <- s[rt][r].
-__device__ __forceinline__ void softmax(Wave& w, float scale_log2, f32x16 (&s)[2], i32x8& ph,
-                                        i32x8& pl) {
+// Raises the rows' maxima to a page's where they lag by more than kLazy, and
+// brings what has been summed to the new ones.
+__device__ __forceinline__ float page_max(const f32x16 (&s)[2]) {
   float mx = s[0][0];
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[rt][r]);
+  return mx;
+}
+__device__ __forceinline__ void raise_max(Wave& w, float mx, float scale_log2) {
   mx = pair_max32(mx) * scale_log2;
-  // -inf - -inf is NaN: no row without keys asks for a new maximum
+  // a row without keys so far takes any maximum; -inf is above nothing
   const bool above = mx > w.m + (w.m == -INFINITY ? 0.f : kLazy);
   if (__any(above)) {
     const float m = above ? mx : w.m;
@@ -225,24 +220,33 @@ __device__ __forceinline__ void softmax(Wave& w, float scale_log2, f32x16 (&s)[2
 #pragma unroll
       for (int r = 0; r < 16; ++r) w.acc[dt][r] *= a;
   }
-  const float off = kLogP - (w.m == -INFINITY ? 0.f : w.m);
-  float l = 0.f;
+}
+__device__ __forceinline__ float exp_offset(const Wave& w) {
+  return kLogP - (w.m == -INFINITY ? 0.f : w.m);
+}
+
+// Softmax numerators of 32 keys, in place, and their leading e4m3 terms:
+// slots 4 at .. 4 at + 15 of the P operand.
+__device__ __forceinline__ void numerators(Wave& w, float scale_log2, float off, f32x16& s,
+                                           i32x8& ph, int at) {
 #pragma unroll
-  for (int rt = 0; rt < 2; ++rt)
+  for (int r = 0; r < 16; r += 4) {
 #pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      float y[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        y[u] = __builtin_amdgcn_exp2f(fmaf(s[rt][r + u], scale_log2, off));
-        l += y[u];
-      }
-      int hi, lo;
-      split4(y, (float)(1 << kRestP), &hi, &lo);
-      ph[4 * rt + r / 4] = hi;
-      pl[4 * rt + r / 4] = lo;
+    for (int u = 0; u < 4; ++u) {
+      s[r + u] = __builtin_amdgcn_exp2f(fmaf(s[r + u], scale_log2, off));
+      w.l += s[r + u];
     }
-  w.l += l;
+    ph[at + r / 4] = cvt4(s[r], s[r + 1], s[r + 2], s[r + 3]);
+  }
+}
+__device__ __forceinline__ i32x8 rests(const f32x16 (&s)[2], const i32x8& ph) {
+  i32x8 pl;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int rt = i >> 2, r = 4 * (i & 3);
+    pl[i] = rest4(s[rt][r], s[rt][r + 1], s[rt][r + 2], s[rt][r + 3], ph[i], (float)(1 << kRestP));
+  }
+  return pl;
 }
 
 // Codes of V at keys at or past `keys` (never written, or left by another
@@ -258,12 +262,39 @@ __device__ __forceinline__ void clear_tail(i32x8 (&vf)[4], int start, int keys) 
   }
 }
 
-__device__ __forceinline__ void add_values(Wave& w, const i32x8 (&vf)[4], const i32x8& ph,
-                                           const i32x8& pl, int sv) {
+// O^T += V^T . P^T of one term of P; rest: log2 of its factor.
+__device__ __forceinline__ void add_values(Wave& w, const i32x8 (&vf)[4], const i32x8& p, int sv,
+                                           int rest) {
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt) w.acc[dt] = SA_MFMA(vf[dt], pl, w.acc[dt], sv, kOne - kRestP);
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt) w.acc[dt] = SA_MFMA(vf[dt], ph, w.acc[dt], sv, kOne);
+  for (int dt = 0; dt < 4; ++dt) w.acc[dt] = SA_MFMA(vf[dt], p, w.acc[dt], sv, kOne - rest);
+}
+
+// 64 pages of a range, one a lane: the pool's page (-1: none) and the E8M0
+// codes of its scales, so that a step needs no load to find them.
+struct PageInfo {
+  int page, scales;
+};
+struct PageAt {  // one of them, uniform
+  int page, sk, sv;
+};
+// Lane i takes table entry first + stride * i, if below `end`.
+__device__ __forceinline__ PageInfo page_info(const CacheIn& c, const int32_t* table, int h, int first,
+                                              int stride, int end) {
+  const int64_t i = first + (int64_t)stride * (threadIdx.x & (kWave - 1));
+  PageInfo f{-1, kOne | (kOne << 8)};
+  if (i < end) {
+    const int page = table[i];
+    if (page >= 0 && page < c.P) {
+      const int64_t at = (int64_t)page * c.Hkv + h;
+      f.page = page;
+      f.scales = e8m0(c.sk[at]) | (e8m0(c.sv[at]) << 8);
+    }
+  }
+  return f;
+}
+__device__ __forceinline__ PageAt page_at(const PageInfo& f, int lane) {
+  const int s = __builtin_amdgcn_readlane(f.scales, lane);
+  return {__builtin_amdgcn_readlane(f.page, lane), s & 0xff, s >> 8};
 }
 
 // Whether a page whose first key is `start` needs the per-score test.
@@ -345,24 +376,30 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Wave w;
   wave_init(p, t, h, t.row0, &w);
-  const table_ptr table = (table_ptr)(p.c.pages + (int64_t)t.b * p.c.pages_stride);
+  const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
 
-  for (int n = from + wave; n < to; n += kWaves) {
-    const int idx = t.page_lo + n;
-    const int page = __builtin_amdgcn_readfirstlane(table[idx]);
-    if (page < 0 || page >= p.c.P) continue;
-    const int64_t at = (int64_t)page * p.c.Hkv + h;
+  PageInfo info;
+  for (int n = from + wave, i = 0; n < to; n += kWaves, ++i) {
+    if ((i & (kWave - 1)) == 0) info = page_info(p.c, table, h, n, kWaves, to);
+    const PageAt pg = page_at(info, i & (kWave - 1));
+    if (pg.page < 0) continue;
+    const int64_t at = ((int64_t)pg.page * p.c.Hkv + h) * kPageBytes;
     i32x8 kf[4], vf[4];
-    load_fragments(kf, p.c.k8 + at * kPageBytes);
-    load_fragments(vf, p.c.v8 + at * kPageBytes);
-    const int start = idx * kPage;
+    load_fragments(kf, p.c.k8 + at);
+    load_fragments(vf, p.c.v8 + at);
+    const int start = (t.page_lo + n) * kPage;
     f32x16 s[2];
-    scores(w, kf, e8m0(((scale_ptr)p.c.sk)[at]), s);
+    s[0] = scores(w, kf[0], kf[1], pg.sk);
+    s[1] = scores(w, kf[2], kf[3], pg.sk);
     if (needs_mask(w, start)) mask_scores(w, start, s);
-    i32x8 ph, pl;
-    softmax(w, p.scale_log2, s, ph, pl);
+    raise_max(w, page_max(s), p.scale_log2);
+    const float off = exp_offset(w);
+    i32x8 ph;
+    numerators(w, p.scale_log2, off, s[0], ph, 0);
+    numerators(w, p.scale_log2, off, s[1], ph, 4);
     if (start + kPage > t.sp.keys) clear_tail(vf, start, t.sp.keys);
-    add_values(w, vf, ph, pl, e8m0(((scale_ptr)p.c.sv)[at]));
+    add_values(w, vf, ph, pg.sv, 0);
+    add_values(w, vf, rests(s, ph), pg.sv, kRestP);
   }
 
   // join the waves: wave i takes channels 32 i .. 32 i + 31
@@ -409,9 +446,37 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
 }
 
 // ---- many rows ----------------------------------------------------------------
+// Pages are copied to LDS up to three ahead, shared by the four waves.  Most
+// pages are seen whole by every row of the tile: they form one range, and go
+// through a loop without masks whose steps interleave matrix and vector work
+// (while S(n + 1) is computed the numerators of page n are taken, while the
+// leading terms of P(n) are multiplied their rests are made, while those are
+// multiplied the maxima of S(n + 1) are taken).  The pages before and after
+// that range (causal borders, the sequence's last page) come first, one by one.
 constexpr int kManyRows = kWaves * kWaveRows;
 constexpr int kManyLeast = 8;
-constexpr int kStages = 3;
+constexpr int kStages = 4;
+
+// `n` times one matrix product, then `v` vector instructions
+#define SA_INTERLEAVE(n, v)                                    \
+  do {                                                         \
+    _Pragma("unroll") for (int i_ = 0; i_ < (n); ++i_) {       \
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       \
+      __builtin_amdgcn_sched_group_barrier(0x002, (v), 0);     \
+    }                                                          \
+  } while (0)
+
+__device__ __forceinline__ i32x8 lds_fragment(const uint8_t* tile, int i) {
+  const uint8_t* s = tile + 2048 * i + 16 * (threadIdx.x & (kWave - 1));
+  const u32x4 lo = ld16(s), hi = ld16(s + 1024);
+  i32x8 f;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    f[y] = (int)lo[y];
+    f[4 + y] = (int)hi[y];
+  }
+  return f;
+}
 
 __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[kStages][2][kPageBytes];
@@ -429,66 +494,175 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   const int lane = threadIdx.x & (kWave - 1);
   Wave w;
   wave_init(p, t, h, t.row0 + kWaveRows * wave, &w);
-  const bool works = t.row0 + kWaveRows * wave < t.rows;
-  const table_ptr table = (table_ptr)(p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo);
+  const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
 
-  // page n of the range into stage n % 3: 2 KB of K and 2 KB of V per wave
-  auto copy = [&](int n) __attribute__((always_inline)) {
-    const int page = __builtin_amdgcn_readfirstlane(table[n]);
-    const bool there = page >= 0 && page < p.c.P;
-    const int64_t at = (there ? (int64_t)page * p.c.Hkv + h : 0) * kPageBytes;
-    const uint32_t to0 = lds0 + (uint32_t)(n % kStages) * (2 * kPageBytes);
+  // pages [mid, end) of the part are seen whole by every row of the tile
+  int mid, end;
+  {
+    int lo, hi, lo1, hi1;
+    visible(p.c, t.sp.pos0 + t.row0 / p.c.g, t.sp.keys, &lo, &hi);
+    visible(p.c, t.sp.pos0 + (min(t.row0 + kManyRows, t.rows) - 1) / p.c.g, t.sp.keys, &lo1, &hi1);
+    mid = min(max((int)(((int64_t)lo1 + kPage - 1) / kPage) - t.page_lo, from), to);
+    end = max(min(hi / kPage - t.page_lo, to), mid);
+  }
+
+  // Whatever is read of a stage that was never copied to must be finite (where
+  // a page is missing its numerators are made zero).
+  for (int i = threadIdx.x; i < (int)sizeof(lds) / 16; i += kThreads)
+    st16(&lds[0][0][0] + 16 * i, (u32x4){0u, 0u, 0u, 0u});
+  __syncthreads();
+
+  // Page n of the part into stage i % 4: 2 KB of K and 2 KB of V per wave, 4
+  // copies a wave (none where there is no page).
+  auto copy = [&](const PageAt& pg, int i) __attribute__((always_inline)) {
+    if (pg.page < 0) return;
+    const int64_t at = ((int64_t)pg.page * p.c.Hkv + h) * kPageBytes;
+    const uint32_t to0 = lds0 + (uint32_t)(i % kStages) * (2 * kPageBytes);
     const auto kr = make_rsrc(p.c.k8 + at, kPageBytes), vr = make_rsrc(p.c.v8 + at, kPageBytes);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t off = (uint32_t)(2 * wave + i) * 1024u;
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t off = (uint32_t)(2 * wave + j) * 1024u;
       dma16(to0 + off, kr, off + 16 * lane, 0);
       dma16(to0 + kPageBytes + off, vr, off + 16 * lane, 0);
     }
   };
-  auto fragments = [&](i32x8 (&f)[4], int n, int kv) __attribute__((always_inline)) {
-    const uint8_t* s = lds[n % kStages][kv];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x4 lo = ld16(s + 2048 * i + 16 * lane), hi = ld16(s + 2048 * i + 1024 + 16 * lane);
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        f[i][y] = (int)lo[y];
-        f[i][4 + y] = (int)hi[y];
-      }
-    }
-  };
-
-  if (from < to) copy(from);
-  if (from + 1 < to) copy(from + 1);
-  for (int n = from; n < to; ++n) {
-    // this wave's copies of page n are done when at most the 4 of page n + 1
-    // are in flight, and its reads of page n - 1 when no LDS read is; the
-    // barrier makes both true of every wave: page n can be read, and page
-    // n + 2 can take the stage of page n - 1
-    if (n + 1 < to)
+  // This wave's copies are done, but for the 4 newest where `newer`, and none
+  // of its LDS reads is in flight; after the barrier both hold for every wave.
+  auto arrive = [&](bool newer) __attribute__((always_inline)) {
+    if (newer)
       asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
     else
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     barrier_keep_loads();
-    const int page = __builtin_amdgcn_readfirstlane(table[n]);
-    if (n + 2 < to) copy(n + 2);
-    if (page < 0 || page >= p.c.P || !works) continue;
-    const int64_t at = (int64_t)page * p.c.Hkv + h;
-    const int start = (t.page_lo + n) * kPage;
-    i32x8 kf[4], vf[4];
-    fragments(kf, n, 0);
-    f32x16 s[2];
-    scores(w, kf, e8m0(((scale_ptr)p.c.sk)[at]), s);
-    if (needs_mask(w, start)) mask_scores(w, start, s);
-    i32x8 ph, pl;
-    softmax(w, p.scale_log2, s, ph, pl);
-    fragments(vf, n, 1);
-    if (start + kPage > t.sp.keys) clear_tail(vf, start, t.sp.keys);
-    add_values(w, vf, ph, pl, e8m0(((scale_ptr)p.c.sv)[at]));
+  };
+  const PageAt none{-1, kOne, kOne};
+
+  auto walk = [&](auto works) __attribute__((always_inline)) {
+    // the border pages: from .. mid - 1, then end .. to - 1
+    const int borders = (mid - from) + (to - end);
+    PageAt pg0 = none, pg1 = none;
+    auto border = [&](int i) __attribute__((always_inline)) {
+      return from + i < mid ? from + i : end + i - (mid - from);
+    };
+    auto border_info = [&](int i) __attribute__((always_inline)) {
+      const int n = border(i);
+      return page_at(page_info(p.c, table, h, n, 0, to), 0);
+    };
+    if (borders > 0) {
+      pg0 = border_info(0);
+      copy(pg0, 0);
+    }
+    for (int i = 0; i < borders; ++i) {
+      arrive(false);  // page i is there, and the other stage free
+      if (i + 1 < borders) {
+        pg1 = border_info(i + 1);
+        copy(pg1, (i + 1) & 1);
+      }
+      if constexpr (works.value) {
+        if (pg0.page >= 0) {
+          const int start = (t.page_lo + border(i)) * kPage;
+          const uint8_t(&tile)[2][kPageBytes] = lds[i & 1];
+          f32x16 s[2];
+#pragma unroll
+          for (int rt = 0; rt < 2; ++rt)
+            s[rt] = scores(w, lds_fragment(tile[0], 2 * rt), lds_fragment(tile[0], 2 * rt + 1), pg0.sk);
+          if (needs_mask(w, start)) mask_scores(w, start, s);
+          raise_max(w, page_max(s), p.scale_log2);
+          const float off = exp_offset(w);
+          i32x8 ph, f[4];
+          numerators(w, p.scale_log2, off, s[0], ph, 0);
+          numerators(w, p.scale_log2, off, s[1], ph, 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = lds_fragment(tile[1], j);
+          if (start + kPage > t.sp.keys) clear_tail(f, start, t.sp.keys);
+          add_values(w, f, ph, pg0.sv, 0);
+          add_values(w, f, rests(s, ph), pg0.sv, kRestP);
+        }
+      }
+      pg0 = pg1;
+    }
+    if (mid >= end) return;
+
+    // the pages seen whole; at step n: pages n .. n + 3
+    PageInfo info = page_info(p.c, table, h, mid, 1, end);
+    auto fetch = [&](int n) __attribute__((always_inline)) {
+      const int i = (n - mid) & (kWave - 1);
+      if (i == 0 && n > mid) info = page_info(p.c, table, h, n, 1, end);
+      const PageAt pg = page_at(info, i);
+      copy(pg, n);
+      return pg;
+    };
+    // the last border page may leave codes past the sequence's end in its
+    // stage: the reads of it are over, and a missing page must not meet them
+    arrive(false);
+    if (borders > 0)
+      for (int i = threadIdx.x; i < 4 * kPageBytes / 16; i += kThreads)
+        st16(&lds[0][0][0] + 16 * i, (u32x4){0u, 0u, 0u, 0u});
+    __syncthreads();
+    PageAt pg2 = none;
+    pg0 = fetch(mid);
+    pg1 = mid + 1 < end ? fetch(mid + 1) : none;
+    arrive(mid + 1 < end && pg1.page >= 0);
+    if (mid + 2 < end) pg2 = fetch(mid + 2);
+    f32x16 sa[2], sb[2];  // scores of the current page and of the next
+    if constexpr (works.value) {
+      const uint8_t* tile = lds[mid % kStages][0];
+      sa[0] = scores(w, lds_fragment(tile, 0), lds_fragment(tile, 1), pg0.sk);
+      sa[1] = scores(w, lds_fragment(tile, 2), lds_fragment(tile, 3), pg0.sk);
+      raise_max(w, pg0.page >= 0 ? page_max(sa) : -INFINITY, p.scale_log2);
+    }
+    auto step = [&](int n, f32x16 (&s)[2], f32x16 (&u)[2]) __attribute__((always_inline)) {
+      arrive(n + 2 < end && pg2.page >= 0);  // page n + 1 is there, and the stage of page n - 1 free
+      PageAt pg3 = none;
+      if (n + 3 < end) pg3 = fetch(n + 3);
+      if constexpr (works.value) {
+        const float off = pg0.page >= 0 ? exp_offset(w) : -INFINITY;
+        const uint8_t* kt = lds[(n + 1) % kStages][0];
+        const uint8_t* vt = lds[n % kStages][1];
+        i32x8 f[4], ph;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = lds_fragment(kt, i);
+        __builtin_amdgcn_sched_barrier(0);
+        u[0] = scores(w, f[0], f[1], pg1.sk);
+        numerators(w, p.scale_log2, off, s[0], ph, 0);
+        SA_INTERLEAVE(4, 14);
+        __builtin_amdgcn_sched_barrier(0);
+        f[0] = lds_fragment(vt, 0);
+        f[1] = lds_fragment(vt, 1);
+        u[1] = scores(w, f[2], f[3], pg1.sk);
+        numerators(w, p.scale_log2, off, s[1], ph, 4);
+        SA_INTERLEAVE(4, 14);
+        __builtin_amdgcn_sched_barrier(0);
+        f[2] = lds_fragment(vt, 2);
+        f[3] = lds_fragment(vt, 3);
+        add_values(w, f, ph, pg0.sv, 0);
+        const i32x8 pl = rests(s, ph);
+        SA_INTERLEAVE(4, 16);
+        __builtin_amdgcn_sched_barrier(0);
+        add_values(w, f, pl, pg0.sv, kRestP);
+        float mx = page_max(u);
+        SA_INTERLEAVE(4, 5);
+        // (taken unconditionally: a branch here would pull the step apart)
+        asm volatile("" : "+v"(mx));
+        __builtin_amdgcn_sched_barrier(0);
+        raise_max(w, n + 1 < end && pg1.page >= 0 ? mx : -INFINITY, p.scale_log2);
+      }
+      pg0 = pg1;
+      pg1 = pg2;
+      pg2 = pg3;
+    };
+    for (int n = mid; n < end; n += 2) {
+      step(n, sa, sb);
+      if (n + 1 < end) step(n + 1, sb, sa);
+    }
+  };
+  if (t.row0 + kWaveRows * wave < t.rows) {
+    walk(std::true_type{});
+  } else {  // no rows: this wave copies its share and keeps the barriers
+    walk(std::false_type{});
+    return;
   }
-  if (!works) return;
   const float l = pair_sum32(w.l);
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) store_channels(p, w, dt, w.acc[dt], l, split, parts == 1);
