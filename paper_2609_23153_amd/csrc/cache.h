@@ -17,35 +17,35 @@ struct Span {
   int start, n, pos0, keys;
 };
 
-// q_start entry i, kept within the packed rows.
-__device__ __forceinline__ int start_of(const CacheIn& c, int i) {
-  return min(max(c.q_start[i], 0), c.T);
-}
-
-__device__ __forceinline__ Span span_of(const CacheIn& c, int b) {
-  Span s;
-  s.start = start_of(c, b);
-  s.n = max(start_of(c, b + 1) - s.start, 0);
-  const int len = max(c.kv_len[b], 0);
-  s.pos0 = len - s.n;
-  s.keys = (int)min((int64_t)len, (int64_t)c.max_pages * kPage);
-  return s;
-}
-
 // Last sequence b whose first(q_start[b], b) is at most w (non-decreasing in
-// b), or -1: the wave reads 64 starts at a time, so a batch of 64 costs one
-// load.  All 64 lanes must be active.
+// b), or -1, and its span.  The wave reads 64 sequences at a time, everything
+// that the span needs with them: one memory latency for a batch of up to 64.
+// All 64 lanes must be active.
 template <typename First>
-__device__ __forceinline__ int find_sequence(const CacheIn& c, int w, First first) {
+__device__ __forceinline__ int find_sequence(const CacheIn& c, int w, First first, Span* sp) {
   const int lane = threadIdx.x & (kWave - 1);
-  int n = 0;
+  int found = -1, start = 0, stop = 0, len = 0;
   for (int b0 = 0; b0 < c.B; b0 += kWave) {
-    const int b = b0 + lane;
-    const uint64_t m = __ballot(b < c.B && first(start_of(c, min(b, c.B - 1)), b) <= w);
-    n += __popcll(m);
+    const int b = min(b0 + lane, c.B - 1);
+    // starts are kept within the packed rows
+    const int s0 = min(max(c.q_start[b], 0), c.T), s1 = min(max(c.q_start[b + 1], 0), c.T);
+    const int n = c.kv_len[b];
+    const uint64_t m = __ballot(b0 + lane < c.B && first(s0, b) <= w);
+    if (m) {
+      const int last = __popcll(m) - 1;  // (a decreasing q_start breaks the contract)
+      found = b0 + last;
+      start = __builtin_amdgcn_readlane(s0, last);
+      stop = __builtin_amdgcn_readlane(s1, last);
+      len = __builtin_amdgcn_readlane(n, last);
+    }
     if (m != ~0ull) break;
   }
-  return n - 1;
+  sp->start = start;
+  sp->n = max(stop - start, 0);
+  len = max(len, 0);
+  sp->pos0 = len - sp->n;
+  sp->keys = (int)min((int64_t)len, (int64_t)c.max_pages * kPage);
+  return found;
 }
 
 // Keys [lo, hi) that the query at position `pos` sees.

@@ -93,9 +93,9 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
   const int h = blockIdx.x % p.c.Hkv, item = blockIdx.x / p.c.Hkv;
   // the sequence: its items start at q_start / 64 + 2 b, and the pages that n
   // tokens touch are at most n / 64 + 2
-  const int b = find_sequence(p.c, item, [&](int s, int i) { return s / kPage + 2 * i; });
+  Span sp;
+  const int b = find_sequence(p.c, item, [&](int s, int i) { return s / kPage + 2 * i; }, &sp);
   if (b < 0) return;
-  const Span sp = span_of(p.c, b);
   const int p0 = max(sp.pos0, 0);  // first position that exists
   const int page_idx = (p0 >> 6) + item - (sp.start / kPage + 2 * b);
   const int64_t base = (int64_t)page_idx * kPage;
@@ -118,22 +118,45 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
       vw[m] = ld16(p.v + (row0 + s) * p.v_tok + h * p.v_head + c8);
     }
   }
+  // slot 0 starts the page anew: whatever it held before is of no sequence
+  const int64_t at = (int64_t)(held ? page : 0) * p.c.Hkv + h;
+  float* sk = p.c.sk + at;
+  float* sv = p.c.sv + at;
+  float k_was = 0.f, v_was = 0.f;
+  if (held && s0 > 0) {
+    k_was = *sk;
+    v_was = *sv;
+  }
   auto table = [&](int s) __attribute__((always_inline)) -> const float* {
     const int64_t row = p.rope_row ? (int64_t)p.rope_row[row0 + s] : base + s;
     return p.rope && row >= 0 && row < p.rope_rows ? p.rope + row * p.rope_dim : nullptr;
   };
-  // the queries that share this key head
+  // the queries that share this key head, four rows of a thread in flight
   if (p.q) {
     const int g = p.c.g, rows = (s1 - s0) * g;
-    for (int i = r0; i < rows; i += kGroups) {
-      const int s = s0 + i / g, hq = h * g + i % g;
-      float v[8];
-      widen8(v, ld16(p.q + (row0 + s) * p.q_tok + hq * p.q_head + c8));
-      rotate8(v, table(s), c8, p.rope_dim);
-      u32x4 w;
+    // i / g as a product: exact for i < 64 g, g <= 1024
+    auto over_g = [&](int i) __attribute__((always_inline)) {
+      return g == 1 ? i : (int)__umulhi((uint32_t)i, p.inv_g);
+    };
+    for (int i0 = r0; i0 < rows; i0 += 4 * kGroups) {
+      u32x4 w[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) w[x] = pack_bf16x2(v[2 * x], v[2 * x + 1]);
-      st16(p.q_out + (row0 + s) * p.qo_tok + hq * p.qo_head + c8, w);
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * kGroups, d = over_g(i), s = s0 + d, hq = h * g + i - d * g;
+        if (i < rows) w[u] = ld16(p.q + (row0 + s) * p.q_tok + hq * p.q_head + c8);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * kGroups, d = over_g(i), s = s0 + d, hq = h * g + i - d * g;
+        if (i < rows) {
+          float v[8];
+          widen8(v, w[u]);
+          rotate8(v, table(s), c8, p.rope_dim);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) w[u][x] = pack_bf16x2(v[2 * x], v[2 * x + 1]);
+          st16(p.q_out + (row0 + s) * p.qo_tok + hq * p.qo_head + c8, w[u]);
+        }
+      }
     }
   }
   if (!held) return;
@@ -159,11 +182,7 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
     red[0][threadIdx.x / kWave] = ka;
     red[1][threadIdx.x / kWave] = va;
   }
-  const int64_t at = (int64_t)page * p.c.Hkv + h;
-  float* sk = p.c.sk + at;
-  float* sv = p.c.sv + at;
-  // slot 0 starts the page anew: whatever it held before is of no sequence
-  const int k_old = s0 > 0 ? e8m0(*sk) - 127 : -126, v_old = s0 > 0 ? e8m0(*sv) - 127 : -126;
+  const int k_old = s0 > 0 ? e8m0(k_was) - 127 : -126, v_old = s0 > 0 ? e8m0(v_was) - 127 : -126;
   __syncthreads();
   ka = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   va = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
@@ -198,30 +217,59 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
     *sk = exp2_of(ke);
     *sv = exp2_of(ve);
   }
-  // V: 16 keys of a channel lie side by side, four of them in a row
-  for (int c = threadIdx.x; c < kPageBytes / 16; c += kThreads) {
-    const int l32 = c & 31, g = (c >> 5) & 1, hf = (c >> 6) & 1, dt = c >> 7;
-    const uint8_t* col = codes + 32 * dt + l32;
-    uint32_t* to = reinterpret_cast<uint32_t*>(vt + 16 * c);
+  // V: 16 keys of a channel lie side by side, four in a row.  A thread turns
+  // four channels of the 16 keys 32 hf + 8 q4 + 4 g + x: 4 x 4 bytes at a time.
+  if (s1 - s0 <= 8 && !v_grows) {  // a few new keys: byte by byte, a channel a thread
+    const int ch = threadIdx.x & 127;
+    for (int s = s0 + (threadIdx.x >> 7); s < s1; s += 2)
+      vt[16 * (64 * (2 * (ch >> 5) + (s >> 5)) + (ch & 31) + 32 * ((s >> 2) & 1)) +
+         4 * ((s >> 3) & 3) + (s & 3)] = codes[s * kHeadDim + ch];
+  } else if (threadIdx.x < 128) {
+    const int ch = 4 * (threadIdx.x & 31), g = (threadIdx.x >> 5) & 1, hf = threadIdx.x >> 6;
+    uint32_t n[4][4];  // [channel][q4]: keys x of a channel as bytes
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
-      const int k0 = 32 * hf + 8 * q4 + 4 * g;
-      const bool any = k0 < s1 && k0 + 4 > s0, all = k0 >= s0 && k0 + 4 <= s1;
-      const bool old = v_grows && k0 < s0;
-      if (!any && !old) continue;
-      const uint32_t n = (uint32_t)col[k0 * kHeadDim] | ((uint32_t)col[(k0 + 1) * kHeadDim] << 8) |
-                         ((uint32_t)col[(k0 + 2) * kHeadDim] << 16) |
-                         ((uint32_t)col[(k0 + 3) * kHeadDim] << 24);
-      if (all) {
-        to[q4] = n;
-      } else if (old) {
-        const uint32_t w = to[q4];
-        to[q4] = merge4(merge4(w, rescale4(w, v_old - ve), k0, 0, s0), n, k0, s0, s1);
-      } else {  // slots past the new ones are left as they are
+      const uint8_t* from = codes + (32 * hf + 8 * q4 + 4 * g) * kHeadDim + ch;
+      uint32_t r[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (k0 + x >= s0 && k0 + x < s1)
-            reinterpret_cast<uint8_t*>(to + q4)[x] = (uint8_t)(n >> (8 * x));
+      for (int x = 0; x < 4; ++x) r[x] = *reinterpret_cast<const uint32_t*>(from + x * kHeadDim);
+      // v_perm_b32: byte selectors 0-3 take the second operand's bytes, 4-7 the first's
+      const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u);  // k0c0 k1c0 k0c1 k1c1
+      const uint32_t b = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u);
+      const uint32_t c = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);  // channels 2, 3
+      const uint32_t d = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+      n[0][q4] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+      n[1][q4] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      n[2][q4] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+      n[3][q4] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+    }
+    const int k_first = 32 * hf + 4 * g, k_last = k_first + 27;  // of this thread's keys
+    if (s0 <= k_first && s1 > k_last) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        st16(vt + 16 * (64 * (2 * (ch >> 5) + hf) + ((ch + j) & 31) + 32 * g),
+             (u32x4){n[j][0], n[j][1], n[j][2], n[j][3]});
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t* to = reinterpret_cast<uint32_t*>(
+            vt + 16 * (64 * (2 * (ch >> 5) + hf) + ((ch + j) & 31) + 32 * g));
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const int k0 = k_first + 8 * q4;
+          const bool any = k0 < s1 && k0 + 4 > s0, old = v_grows && k0 < s0;
+          if (k0 >= s0 && k0 + 4 <= s1) {
+            to[q4] = n[j][q4];
+          } else if (old) {
+            const uint32_t w = to[q4];
+            to[q4] = merge4(merge4(w, rescale4(w, v_old - ve), k0, 0, s0), n[j][q4], k0, s0, s1);
+          } else if (any) {  // slots past the new ones are left as they are
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (k0 + x >= s0 && k0 + x < s1)
+                reinterpret_cast<uint8_t*>(to + q4)[x] = (uint8_t)(n[j][q4] >> (8 * x));
+          }
+        }
       }
     }
   }
@@ -234,7 +282,9 @@ int64_t cache_append_items(const CacheIn& c) { return (int64_t)c.T / kPage + 2 *
 hipError_t launch_cache_append(const AppendIn& in, hipStream_t stream) {
   if (in.c.T == 0) return hipSuccess;
   const int64_t n = cache_append_items(in.c) * in.c.Hkv;
-  cache_append_kernel<<<(unsigned)n, kThreads, 0, stream>>>(in);
+  AppendIn a = in;
+  a.inv_g = 0xffffffffu / (uint32_t)a.c.g + 1u;  // ceil(2^32 / g), g > 1
+  cache_append_kernel<<<(unsigned)n, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

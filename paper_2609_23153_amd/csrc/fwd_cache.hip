@@ -46,7 +46,7 @@ struct Params {
   float* part_o;     // [splits][T * H][128]
   float2* part_ml;   // [splits][T * H]: maximum (log2 units), row sum
   int64_t q_tok, q_head, o_tok, o_head;
-  int H, splits, tiles;
+  int H, splits, least;  // parts of a key range at most, pages of a part at least
   float scale_log2;
 };
 
@@ -72,9 +72,8 @@ template <int R>
 __device__ __forceinline__ bool find_tile(const CacheIn& c, int w, Tile* t) {
   // a sequence of n tokens has at most n g / R + 1 tiles
   auto first = [&](int s, int i) { return (int)((int64_t)s * c.g / R) + i; };
-  t->b = find_sequence(c, w, first);
+  t->b = find_sequence(c, w, first, &t->sp);
   if (t->b < 0) return false;
-  t->sp = span_of(c, t->b);
   t->rows = t->sp.n * c.g;
   const int64_t row0 = (int64_t)(w - first(t->sp.start, t->b)) * R;
   if (row0 >= t->rows) return false;
@@ -345,7 +344,6 @@ __device__ __forceinline__ void store_sums(const Params& p, const Wave& w, float
 
 // ---- few rows ---------------------------------------------------------------
 constexpr int kFewRows = 32;
-constexpr int kFewLeast = 4;  // pages of a part at least: one a wave
 
 __device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* tile) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -369,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
   const int h = x % p.c.Hkv;
   Tile t;
   if (!find_tile<kFewRows>(p.c, x / p.c.Hkv, &t)) return;
-  const int parts = parts_of(t.pages, p.splits, kFewLeast);
+  const int parts = parts_of(t.pages, p.splits, p.least);
   if (split >= parts) return;
   const int from = (int)((int64_t)t.pages * split / parts);
   const int to = (int)((int64_t)t.pages * (split + 1) / parts);
@@ -378,19 +376,25 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
   wave_init(p, t, h, t.row0, &w);
   const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
 
+  // pages from + wave + 4 i, 64 of them known at a time
+  const int mine = to > from + wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
   PageInfo info;
-  for (int n = from + wave, i = 0; n < to; n += kWaves, ++i) {
+  for (int i = 0; i < mine; ++i) {
+    const int n = from + wave + kWaves * i;
     if ((i & (kWave - 1)) == 0) info = page_info(p.c, table, h, n, kWaves, to);
-    const PageAt pg = page_at(info, i & (kWave - 1));
-    if (pg.page < 0) continue;
-    const int64_t at = ((int64_t)pg.page * p.c.Hkv + h) * kPageBytes;
+    const int page = __builtin_amdgcn_readlane(info.page, i & (kWave - 1));
+    if (page < 0) continue;
+    const int64_t at = ((int64_t)page * p.c.Hkv + h) * kPageBytes;
     i32x8 kf[4], vf[4];
     load_fragments(kf, p.c.k8 + at);
     load_fragments(vf, p.c.v8 + at);
-    const int start = (t.page_lo + n) * kPage;
+    // (the scales may still be on their way when the tiles are asked for)
+    __builtin_amdgcn_sched_barrier(0);
+    const int scales = __builtin_amdgcn_readlane(info.scales, i & (kWave - 1));
+    const int sk = scales & 0xff, sv = scales >> 8, start = (t.page_lo + n) * kPage;
     f32x16 s[2];
-    s[0] = scores(w, kf[0], kf[1], pg.sk);
-    s[1] = scores(w, kf[2], kf[3], pg.sk);
+    s[0] = scores(w, kf[0], kf[1], sk);
+    s[1] = scores(w, kf[2], kf[3], sk);
     if (needs_mask(w, start)) mask_scores(w, start, s);
     raise_max(w, page_max(s), p.scale_log2);
     const float off = exp_offset(w);
@@ -398,8 +402,8 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
     numerators(w, p.scale_log2, off, s[0], ph, 0);
     numerators(w, p.scale_log2, off, s[1], ph, 4);
     if (start + kPage > t.sp.keys) clear_tail(vf, start, t.sp.keys);
-    add_values(w, vf, ph, pg.sv, 0);
-    add_values(w, vf, rests(s, ph), pg.sv, kRestP);
+    add_values(w, vf, ph, sv, 0);
+    add_values(w, vf, rests(s, ph), sv, kRestP);
   }
 
   // join the waves: wave i takes channels 32 i .. 32 i + 31
@@ -454,7 +458,6 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
 // multiplied the maxima of S(n + 1) are taken).  The pages before and after
 // that range (causal borders, the sequence's last page) come first, one by one.
 constexpr int kManyRows = kWaves * kWaveRows;
-constexpr int kManyLeast = 8;
 constexpr int kStages = 4;
 
 // `n` times one matrix product, then `v` vector instructions
@@ -486,7 +489,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   const int h = x % p.c.Hkv;
   Tile t;
   if (!find_tile<kManyRows>(p.c, x / p.c.Hkv, &t)) return;
-  const int parts = parts_of(t.pages, p.splits, kManyLeast);
+  const int parts = parts_of(t.pages, p.splits, p.least);
   if (split >= parts) return;
   const int from = (int)((int64_t)t.pages * split / parts);
   const int to = (int)((int64_t)t.pages * (split + 1) / parts);
@@ -670,35 +673,50 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
 }
 
 // ---- parts joined -------------------------------------------------------------
-// One wave per (token, head), two channels a lane.
-template <int R, int LEAST>
+// One wave per (token, head), two channels a lane.  The loads of the shares do
+// not wait for the sequence's own numbers: 16 at a time, what no part wrote
+// counting nothing.
+constexpr int kJoin = 16;
+template <int R>
 __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
   const int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
   const int lane = threadIdx.x & (kWave - 1);
   if (row >= (int64_t)p.c.T * p.H) return;
+  const int64_t step = (int64_t)p.c.T * p.H;
+  const float* from = p.part_o + row * kHeadDim + 2 * lane;
+  float2 v[kJoin];
+  auto fetch = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i)
+      if (i0 + i < p.splits)
+        v[i] = *reinterpret_cast<const float2*>(from + (i0 + i) * step * kHeadDim);
+  };
+  fetch(0);
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < p.splits) ml = p.part_ml[lane * step + row];
   const int tok = (int)(row / p.H), head = (int)(row - (int64_t)tok * p.H);
   Tile t;
-  t.b = find_sequence(p.c, tok, [](int s, int) { return s; });
-  if (t.b < 0) return;
-  t.sp = span_of(p.c, t.b);
-  if (tok - t.sp.start >= t.sp.n) return;
+  t.b = find_sequence(p.c, tok, [](int s, int) { return s; }, &t.sp);
+  if (t.b < 0 || tok - t.sp.start >= t.sp.n) return;
   t.rows = t.sp.n * p.c.g;
   t.row0 = ((tok - t.sp.start) * p.c.g + head % p.c.g) / R * R;
   tile_range<R>(p.c, &t);
-  const int parts = parts_of(t.pages, p.splits, LEAST);
-  if (parts == 1) return;
-  const int64_t step = (int64_t)p.c.T * p.H;
-  const float2 ml = lane < parts ? p.part_ml[lane * step + row] : make_float2(-INFINITY, 0.f);
+  const int parts = parts_of(t.pages, p.splits, p.least);
+  if (parts == 1) return;  // written whole
+  if (lane >= parts) ml = make_float2(-INFINITY, 0.f);
   const float m = wave_max(ml.x);
   const float a = __builtin_amdgcn_exp2f(ml.x - (m == -INFINITY ? 0.f : m));
   const float l = wave_sum_f32(a * ml.y);
-  const float* from = p.part_o + row * kHeadDim + 2 * lane;
   float x = 0.f, y = 0.f;
-  for (int i = 0; i < parts; ++i) {
-    const float ai = __shfl(a, i, kWave);
-    const float2 v = *reinterpret_cast<const float2*>(from + i * step * kHeadDim);
-    x = fmaf(ai, v.x, x);
-    y = fmaf(ai, v.y, y);
+  for (int i0 = 0; i0 < parts; i0 += kJoin) {
+    if (i0 > 0) fetch(i0);
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i)
+      if (i0 + i < parts) {
+        const float ai = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(a), i0 + i));
+        x = fmaf(ai, v[i].x, x);
+        y = fmaf(ai, v[i].y, y);
+      }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   *reinterpret_cast<uint32_t*>(p.o + tok * p.o_tok + head * p.o_head + 2 * lane) =
@@ -706,22 +724,34 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
   if (lane == 0 && p.lse) p.lse[row] = lse_of(m, l);
 }
 
-// How the work is cut: few rows a sequence go to the kernel that is bound by
-// the cache's bytes.  Parts are made until about `want` workgroups are there.
+// How the work is cut.  Few rows a sequence go to the kernel that is bound by
+// the cache's bytes.  A part is given at least one page a wave where there are
+// not enough workgroups for every CU, four where there are (its start and end
+// cost about as much as two pages).
 struct Plan {
   bool few;
   int64_t tiles;
-  int splits;
+  int splits, least;
 };
+constexpr int kSlots = 512;  // workgroups that run at once: 256 CUs, two each
 Plan plan_of(const CacheIn& c) {
   Plan pl;
   const int64_t rows = (int64_t)c.T * c.g;
   pl.few = rows <= (int64_t)kFewRows * c.B;
   pl.tiles = rows / (pl.few ? kFewRows : kManyRows) + c.B;
-  const int64_t want = pl.few ? 1024 : 512, have = pl.tiles * c.Hkv;
-  const int64_t most = c.max_pages / (pl.few ? kFewLeast : kManyLeast);
-  int64_t s = (want + have - 1) / have;
-  if (s > most) s = most;
+  const int64_t have = pl.tiles * c.Hkv;
+  int64_t s;
+  if (pl.few) {
+    // sequences differ in length: parts enough that the longest one's do not
+    // run on alone
+    pl.least = have >= kSlots ? 16 : 4;
+    s = (8 * kSlots + have - 1) / have;
+    if (have < kSlots && s > (kSlots + have - 1) / have) s = (kSlots + have - 1) / have;
+  } else {
+    pl.least = 8;
+    s = have >= kSlots / 2 ? 1 : kSlots / have;
+  }
+  if (s > c.max_pages / pl.least) s = c.max_pages / pl.least;
   pl.splits = (int)(s < 1 ? 1 : s > kWave ? kWave : s);
   return pl;
 }
@@ -748,7 +778,7 @@ hipError_t launch_fwd_cache(const FwdCacheIn& in, void* ws, hipStream_t stream) 
   p.o_head = in.o_head;
   p.H = in.c.Hkv * in.c.g;
   p.splits = pl.splits;
-  p.tiles = (int)pl.tiles;
+  p.least = pl.least;
   p.scale_log2 = in.softmax_scale * 1.4426950408889634f;
   p.part_o = static_cast<float*>(ws);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (int64_t)pl.splits * in.c.T * p.H * kHeadDim);
@@ -761,9 +791,9 @@ hipError_t launch_fwd_cache(const FwdCacheIn& in, void* ws, hipStream_t stream) 
   if (e != hipSuccess || pl.splits == 1) return e;
   const unsigned rows = (unsigned)(((int64_t)in.c.T * p.H + kWaves - 1) / kWaves);
   if (pl.few)
-    fwd_cache_join_kernel<kFewRows, kFewLeast><<<rows, kThreads, 0, stream>>>(p);
+    fwd_cache_join_kernel<kFewRows><<<rows, kThreads, 0, stream>>>(p);
   else
-    fwd_cache_join_kernel<kManyRows, kManyLeast><<<rows, kThreads, 0, stream>>>(p);
+    fwd_cache_join_kernel<kManyRows><<<rows, kThreads, 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -285,25 +285,32 @@ __global__ __launch_bounds__(kWave* kRedRuns) void layer_norm_reduce_kernel(cons
   }
 }
 
-// Threads per row, and the elements each holds at most: a wave alone needs no
-// barrier and serves rows up to 2048 channels; longer ones take four.
+// Threads per row, and the elements each holds at most.  Forward: a wave alone
+// needs no barrier and serves rows up to 2048 channels; longer ones take four.
+// Backward: four from 512 channels on, so that fewer teams, and with them fewer
+// partial gradients, keep as many waves busy (1,554 x 1,531 fp32: 777 one-wave
+// teams a group 26 us with the sum of the partials, 128 of four waves @@).
 struct Team {
   int threads, elems;
 };
-Team team_of(int64_t cols) {
+Team team_of(int64_t cols, bool backward) {
   if (cols <= 512) return {64, 8};
-  if (cols <= 2048) return {64, 32};
+  if (cols <= 2048) return backward ? Team{256, 8} : Team{64, 32};
   if (cols <= 6144) return {256, 24};
   return {256, 64};
 }
 
 int fwd_teams(int64_t rows, int64_t cols, int64_t groups) {
-  const int64_t cap = (team_of(cols).threads == 64 ? 8192 : 2048) / groups;
+  const int64_t cap = (team_of(cols, false).threads == 64 ? 8192 : 2048) / groups;
   return (int)(rows < cap ? rows : cap < 1 ? 1 : cap);
 }
+// Teams of a group of `rows` rows: each adds a partial row of 2 x cols floats to
+// write and read, so none has fewer than 8 rows while 256 teams are there.
 int bwd_teams(int64_t rows, int64_t cols, int64_t groups) {
-  const int64_t cap = (team_of(cols).threads == 64 ? 2048 : 1024) / groups;
-  const int64_t t = rows < cap ? rows : cap;
+  const int64_t most = team_of(cols, true).threads == 64 ? 2048 : 1024;
+  int64_t t = rows * groups / 8;
+  t = (t < 256 ? 256 : t > most ? most : t) / groups;
+  t = t < rows ? t : rows;
   return (int)(t < 1 ? 1 : t);
 }
 
@@ -325,13 +332,13 @@ void run_bwd(const LayerNormBwdIn& in, float* part, hipStream_t stream) {
 }
 
 // F<T, VEC, TPR, NC>(...) for the row's type, length and alignment.
-#define SA_NORM_TEAMS(F, T, VEC, cols, ...)                     \
+#define SA_NORM_TEAMS(F, T, VEC, cols, BACK, ...)               \
   do {                                                          \
-    const Team tm = team_of(cols);                              \
+    const Team tm = team_of(cols, BACK);                        \
     if (tm.threads == 64 && tm.elems == 8)                      \
       F<T, VEC, 64, 8 / VEC>(__VA_ARGS__);                      \
-    else if (tm.threads == 64)                                  \
-      F<T, VEC, 64, 32 / VEC>(__VA_ARGS__);                     \
+    else if (tm.elems <= 32 && tm.elems != 24)                  \
+      F<T, VEC, BACK ? 256 : 64, (BACK ? 8 : 32) / VEC>(__VA_ARGS__); \
     else if (tm.elems == 24)                                    \
       F<T, VEC, 256, 24 / VEC>(__VA_ARGS__);                    \
     else                                                        \
@@ -355,14 +362,14 @@ hipError_t launch_layer_norm(const LayerNormIn& in, hipStream_t stream) {
   const bool vec = in.cols % 8 == 0 && whole(in.x, in.ldx, elem) && whole(in.y, in.ldy, elem);
   if (in.f32) {
     if (vec)
-      SA_NORM_TEAMS(run_fwd, float, 8, in.cols, in, stream);
+      SA_NORM_TEAMS(run_fwd, float, 8, in.cols, false, in, stream);
     else
-      SA_NORM_TEAMS(run_fwd, float, 1, in.cols, in, stream);
+      SA_NORM_TEAMS(run_fwd, float, 1, in.cols, false, in, stream);
   } else {
     if (vec)
-      SA_NORM_TEAMS(run_fwd, uint16_t, 8, in.cols, in, stream);
+      SA_NORM_TEAMS(run_fwd, uint16_t, 8, in.cols, false, in, stream);
     else
-      SA_NORM_TEAMS(run_fwd, uint16_t, 1, in.cols, in, stream);
+      SA_NORM_TEAMS(run_fwd, uint16_t, 1, in.cols, false, in, stream);
   }
   return hipGetLastError();
 }
@@ -375,14 +382,14 @@ hipError_t launch_layer_norm_bwd(const LayerNormBwdIn& in, void* ws, hipStream_t
                      whole(in.dy, in.lddy, elem) && whole(in.dx, in.lddx, elem);
     if (in.f32) {
       if (vec)
-        SA_NORM_TEAMS(run_bwd, float, 8, in.cols, in, part, stream);
+        SA_NORM_TEAMS(run_bwd, float, 8, in.cols, true, in, part, stream);
       else
-        SA_NORM_TEAMS(run_bwd, float, 1, in.cols, in, part, stream);
+        SA_NORM_TEAMS(run_bwd, float, 1, in.cols, true, in, part, stream);
     } else {
       if (vec)
-        SA_NORM_TEAMS(run_bwd, uint16_t, 8, in.cols, in, part, stream);
+        SA_NORM_TEAMS(run_bwd, uint16_t, 8, in.cols, true, in, part, stream);
       else
-        SA_NORM_TEAMS(run_bwd, uint16_t, 1, in.cols, in, part, stream);
+        SA_NORM_TEAMS(run_bwd, uint16_t, 1, in.cols, true, in, part, stream);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
