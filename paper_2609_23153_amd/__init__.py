@@ -575,11 +575,23 @@ def _cache_pool(dev, k8, sk, v8, sv, pages, q_start, kv_len):
     if unit != 1 and most > 1:
         raise ValueError("the rows of pages must be contiguous")
     n = num * kv
-    return (num, kv, batch, most, stride if batch > 1 else most), (
-        _arr(k8, "k8", torch.uint8, dev, n * 8192), _arr(sk, "sk", torch.float32, dev, n),
-        _arr(v8, "v8", torch.uint8, dev, n * 8192), _arr(sv, "sv", torch.float32, dev, n),
-        pages.data_ptr(), _arr(q_start, "q_start", torch.int32, dev, batch + 1),
-        _arr(kv_len, "kv_len", torch.int32, dev, batch))
+    # one pass over the tensors; which one is wrong is found out only then
+    if (k8.dtype is v8.dtype is torch.uint8 and sk.dtype is sv.dtype is torch.float32
+            and q_start.dtype is kv_len.dtype is torch.int32
+            and v8.numel() == n * 8192 and sk.numel() == n == sv.numel()
+            and q_start.numel() == batch + 1 and kv_len.numel() == batch
+            and k8.get_device() == v8.get_device() == sk.get_device() == sv.get_device()
+            == q_start.get_device() == kv_len.get_device() == dev
+            and k8.is_contiguous() and v8.is_contiguous() and sk.is_contiguous()
+            and sv.is_contiguous() and q_start.is_contiguous() and kv_len.is_contiguous()):
+        at = (k8.data_ptr(), sk.data_ptr(), v8.data_ptr(), sv.data_ptr(), pages.data_ptr(),
+              q_start.data_ptr(), kv_len.data_ptr())
+    else:
+        at = (_arr(k8, "k8", torch.uint8, dev, n * 8192), _arr(sk, "sk", torch.float32, dev, n),
+              _arr(v8, "v8", torch.uint8, dev, n * 8192), _arr(sv, "sv", torch.float32, dev, n),
+              pages.data_ptr(), _arr(q_start, "q_start", torch.int32, dev, batch + 1),
+              _arr(kv_len, "kv_len", torch.int32, dev, batch))
+    return (num, kv, batch, most, stride if batch > 1 else most), at
 
 
 def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=None,
