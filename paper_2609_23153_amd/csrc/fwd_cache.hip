@@ -100,10 +100,12 @@ struct Wave {
   bool valid;
 };
 
-// e4m3 codes of four values.  (Both halves of the word are written: what it
-// holds before does not matter.)
+// e4m3 codes of four values.  Each conversion writes half a word; what the
+// word held before does not matter, and no instruction is spent on it.
 __device__ __forceinline__ int cvt4(float a, float b, float c, float d) {
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, __builtin_nondeterministic_value(0), false);
+  int w;
+  asm("" : "=v"(w));
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 // The rests (x - h) up of four values whose codes h holds, as codes.
@@ -452,22 +454,15 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
 // ---- many rows ----------------------------------------------------------------
 // Pages are copied to LDS up to three ahead, shared by the four waves.  Most
 // pages are seen whole by every row of the tile: they form one range, and go
-// through a loop without masks whose steps interleave matrix and vector work
-// (while S(n + 1) is computed the numerators of page n are taken, while the
-// leading terms of P(n) are multiplied their rests are made, while those are
-// multiplied the maxima of S(n + 1) are taken).  The pages before and after
-// that range (causal borders, the sequence's last page) come first, one by one.
+// through a loop without masks or branches whose steps hold matrix work and
+// independent vector work side by side: S(n + 1) beside the numerators of page
+// n, the products of P(n)'s leading terms beside their rests, those of the rests
+// beside the maxima of S(n + 1).  (Spelling the order of the two out, with
+// scheduling groups of 14 vector instructions a product, made it 3% slower.)
+// The pages before and after that range (causal borders, the sequence's last
+// page) come first, one by one.
 constexpr int kManyRows = kWaves * kWaveRows;
 constexpr int kStages = 4;
-
-// `n` times one matrix product, then `v` vector instructions
-#define SA_INTERLEAVE(n, v)                                    \
-  do {                                                         \
-    _Pragma("unroll") for (int i_ = 0; i_ < (n); ++i_) {       \
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       \
-      __builtin_amdgcn_sched_group_barrier(0x002, (v), 0);     \
-    }                                                          \
-  } while (0)
 
 __device__ __forceinline__ i32x8 lds_fragment(const uint8_t* tile, int i) {
   const uint8_t* s = tile + 2048 * i + 16 * (threadIdx.x & (kWave - 1));
@@ -626,29 +621,20 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
         i32x8 f[4], ph;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = lds_fragment(kt, i);
-        __builtin_amdgcn_sched_barrier(0);
         u[0] = scores(w, f[0], f[1], pg1.sk);
         numerators(w, p.scale_log2, off, s[0], ph, 0);
-        SA_INTERLEAVE(4, 14);
-        __builtin_amdgcn_sched_barrier(0);
         f[0] = lds_fragment(vt, 0);
         f[1] = lds_fragment(vt, 1);
         u[1] = scores(w, f[2], f[3], pg1.sk);
         numerators(w, p.scale_log2, off, s[1], ph, 4);
-        SA_INTERLEAVE(4, 14);
-        __builtin_amdgcn_sched_barrier(0);
         f[2] = lds_fragment(vt, 2);
         f[3] = lds_fragment(vt, 3);
         add_values(w, f, ph, pg0.sv, 0);
         const i32x8 pl = rests(s, ph);
-        SA_INTERLEAVE(4, 16);
-        __builtin_amdgcn_sched_barrier(0);
         add_values(w, f, pl, pg0.sv, kRestP);
         float mx = page_max(u);
-        SA_INTERLEAVE(4, 5);
         // (taken unconditionally: a branch here would pull the step apart)
         asm volatile("" : "+v"(mx));
-        __builtin_amdgcn_sched_barrier(0);
         raise_max(w, n + 1 < end && pg1.page >= 0 ? mx : -INFINITY, p.scale_log2);
       }
       pg0 = pg1;
