@@ -361,7 +361,7 @@ __device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* til
 }
 
 __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
-  __shared__ __attribute__((aligned(16))) float xo[kWaves][kWaves - 1][16][kWave];
+  __shared__ __attribute__((aligned(16))) float xo[kWaves][kWaves - 1][4][kWave][4];
   __shared__ float xm[kWaves][kWaveRows], xl[kWaves][kWaveRows];
   int x = blockIdx.x;
   const int split = x % p.splits;
@@ -419,7 +419,9 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
   for (int dt = 0; dt < kWaves; ++dt)
     if (dt != wave) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) xo[dt][wave < dt ? wave : wave - 1][r][lane] = w.acc[dt][r];
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4*>(xo[dt][wave < dt ? wave : wave - 1][r][lane]) =
+            (f32x4){w.acc[dt][4 * r], w.acc[dt][4 * r + 1], w.acc[dt][4 * r + 2], w.acc[dt][4 * r + 3]};
     }
   __syncthreads();
   float m = xm[0][l32];
@@ -436,17 +438,21 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) sum[r] = 0.f;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
+  for (int dt = 0; dt < kWaves; ++dt)
+    if (dt == wave) {
 #pragma unroll
-    for (int dt = 0; dt < kWaves; ++dt)
-      if (dt == wave) {
+      for (int i = 0; i < kWaves; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float v = i == dt ? w.acc[dt][r] : xo[dt][i < dt ? i : i - 1][r][lane];
-          sum[r] = fmaf(a[i], v, sum[r]);
+        for (int r = 0; r < 4; ++r) {
+          f32x4 v;
+          if (i == dt)
+            v = (f32x4){w.acc[dt][4 * r], w.acc[dt][4 * r + 1], w.acc[dt][4 * r + 2], w.acc[dt][4 * r + 3]};
+          else
+            v = *reinterpret_cast<const f32x4*>(xo[dt][i < dt ? i : i - 1][r][lane]);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) sum[4 * r + y] = fmaf(a[i], v[y], sum[4 * r + y]);
         }
-      }
-  }
+    }
   store_channels(p, w, wave, sum, l, split, parts == 1);
   if (wave == 0) store_sums(p, w, m, l, split, parts == 1);
 }

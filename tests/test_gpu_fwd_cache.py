@@ -137,6 +137,23 @@ def test_more_than_a_wave_of_sequences():
     run(lengths, [min(n, 1 + i % 2) for i, n in enumerate(lengths)], 1, 2)
 
 
+@pytest.mark.parametrize("chunk,window", [(0, 0), (1, 0), (1, 130), (5, 3), (300, 1)])
+@pytest.mark.parametrize("g,most", [(3, 4), (8, 9), (1, 60)])
+def test_equal_shares_of_ragged_long_caches(g, most, chunk, window):
+    # several tiles a sequence, sequences without tokens or keys, more than 64 of
+    # them, lengths from none to 2,000: shares begin and end anywhere
+    rng = np.random.default_rng(most)
+    lengths = [0, 2000] + np.exp(rng.uniform(0, 7.6, 68)).astype(int).tolist() + [0, 0]
+    new = [min(n, int(rng.integers(0, most))) for n in lengths]
+    run(lengths, new, 2, g, chunk, window, seed=3, front=1, back=2)
+
+
+@pytest.mark.parametrize("kv", [1, 2, 9])
+def test_one_long_sequence_in_many_parts(kv):
+    run([40000], [1], kv, 2, seed=5)
+    run([64, 9000, 1], [1, 3, 1], kv, 2, 1, 0, seed=6)
+
+
 def test_large_scores_and_a_late_maximum():
     # logits spread over hundreds: later pages move the maximum far, most
     # probabilities vanish
