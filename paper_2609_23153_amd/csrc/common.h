@@ -64,6 +64,11 @@ __device__ __forceinline__ void barrier_keep_loads() { asm volatile("s_barrier" 
 __device__ __forceinline__ u32x4 ld16(const void* p) {
   return *reinterpret_cast<const u32x4*>(p);
 }
+// The same for data that is read once: it does not push out what the caches
+// hold (one token over a long cache: 5.5 -> 6.2 TB/s).
+__device__ __forceinline__ u32x4 ld16_once(const void* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+}
 __device__ __forceinline__ void st16(void* p, u32x4 v) { *reinterpret_cast<u32x4*>(p) = v; }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }

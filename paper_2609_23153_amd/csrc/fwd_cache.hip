@@ -351,7 +351,8 @@ __device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* til
   const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const u32x4 lo = ld16(tile + 2048 * i + 16 * lane), hi = ld16(tile + 2048 * i + 1024 + 16 * lane);
+    const u32x4 lo = ld16_once(tile + 2048 * i + 16 * lane);
+    const u32x4 hi = ld16_once(tile + 2048 * i + 1024 + 16 * lane);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       f[i][x] = (int)lo[x];

@@ -11,6 +11,8 @@
 // next row's loads in flight.  Every statistic and sum is fp32.  The weights'
 // gradients leave a team as one partial row each, which a second kernel adds
 // in a fixed order: no atomics, the same bits every time.
+#include <type_traits>
+
 #include "common.h"
 #include "launch.h"
 
@@ -19,13 +21,26 @@ namespace {
 
 constexpr int kMaxTeamWaves = 4;
 
+// 16 bytes; ONCE: data too large for the caches, which it is then kept out of.
+template <bool ONCE>
+__device__ __forceinline__ u32x4 piece_ld(const void* p) {
+  return ONCE ? ld16_once(p) : ld16(p);
+}
+template <bool ONCE>
+__device__ __forceinline__ void piece_st(void* p, u32x4 v) {
+  if (ONCE)
+    __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else
+    st16(p, v);
+}
+
 // VEC consecutive elements of a row as loaded, and their fp32 values.
-template <typename T, int VEC>
+template <typename T, int VEC, bool ONCE>
 struct Piece;
-template <>
-struct Piece<uint16_t, 8> {
+template <bool ONCE>
+struct Piece<uint16_t, 8, ONCE> {
   u32x4 a;
-  __device__ __forceinline__ void load(const uint16_t* p) { a = ld16(p); }
+  __device__ __forceinline__ void load(const uint16_t* p) { a = piece_ld<ONCE>(p); }
   __device__ __forceinline__ float get(int e) const {
     return (e & 1) ? bf16_hi(a[e >> 1]) : bf16_lo(a[e >> 1]);
   }
@@ -33,24 +48,29 @@ struct Piece<uint16_t, 8> {
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    st16(p, w);
+    piece_st<ONCE>(p, w);
   }
 };
-template <>
-struct Piece<float, 8> {
-  f32x4 a, b;
+template <bool ONCE>
+struct Piece<float, 8, ONCE> {
+  u32x4 a, b;
   __device__ __forceinline__ void load(const float* p) {
-    a = *reinterpret_cast<const f32x4*>(p);
-    b = *reinterpret_cast<const f32x4*>(p + 4);
+    a = piece_ld<ONCE>(p);
+    b = piece_ld<ONCE>(p + 4);
   }
-  __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
+  __device__ __forceinline__ float get(int e) const {
+    return __uint_as_float(e < 4 ? a[e & 3] : b[e & 3]);
+  }
   static __device__ __forceinline__ void store(float* p, const float* v) {
-    *reinterpret_cast<f32x4*>(p) = (f32x4){v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = (f32x4){v[4], v[5], v[6], v[7]};
+    u32x4 w[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = __float_as_uint(v[i]);
+    piece_st<ONCE>(p, w[0]);
+    piece_st<ONCE>(p + 4, w[1]);
   }
 };
 template <>
-struct Piece<uint16_t, 1> {
+struct Piece<uint16_t, 1, false> {
   uint16_t a;
   __device__ __forceinline__ void load(const uint16_t* p) { a = *p; }
   __device__ __forceinline__ float get(int) const { return __uint_as_float((uint32_t)a << 16); }
@@ -59,7 +79,7 @@ struct Piece<uint16_t, 1> {
   }
 };
 template <>
-struct Piece<float, 1> {
+struct Piece<float, 1, false> {
   float a;
   __device__ __forceinline__ void load(const float* p) { a = *p; }
   __device__ __forceinline__ float get(int) const { return a; }
@@ -78,11 +98,11 @@ __device__ __forceinline__ void load_weights(float (&w)[NC][VEC], const float* p
   }
 }
 
-template <typename T, int VEC, int TPR, int NC>
+template <typename T, int VEC, bool ONCE, int TPR, int NC>
 __global__ __launch_bounds__(TPR) void layer_norm_kernel(
     const T* x, int64_t ldx, int64_t rows, int cols, const float* weight, const float* bias,
     float eps, T* y, int64_t ldy, float* mean_out, float* rstd_out) {
-  using P = Piece<T, VEC>;
+  using P = Piece<T, VEC, ONCE>;
   constexpr int kWaves = TPR / kWave;
   const int tid = threadIdx.x, wave = tid / kWave;
   const int64_t first = (int64_t)blockIdx.y * rows;  // first row of the group
@@ -167,11 +187,11 @@ __global__ __launch_bounds__(TPR) void layer_norm_kernel(
   }
 }
 
-template <typename T, int VEC, int TPR, int NC>
+template <typename T, int VEC, bool ONCE, int TPR, int NC>
 __global__ __launch_bounds__(TPR) void layer_norm_bwd_kernel(
     const T* dy, int64_t lddy, const T* x, int64_t ldx, const float* mean, const float* rstd,
     int64_t rows, int cols, const float* weight, T* dx, int64_t lddx, float* part) {
-  using P = Piece<T, VEC>;
+  using P = Piece<T, VEC, ONCE>;
   constexpr int kWaves = TPR / kWave;
   const int tid = threadIdx.x, wave = tid / kWave;
   const int64_t first = (int64_t)blockIdx.y * rows;
@@ -289,7 +309,7 @@ __global__ __launch_bounds__(kWave* kRedRuns) void layer_norm_reduce_kernel(cons
 // needs no barrier and serves rows up to 2048 channels; longer ones take four.
 // Backward: four from 512 channels on, so that fewer teams, and with them fewer
 // partial gradients, keep as many waves busy (1,554 x 1,531 fp32: 777 one-wave
-// teams a group 26 us with the sum of the partials, 128 of four waves @@).
+// teams a group 26 us with the sum of the partials, 128 of four waves 18.5).
 struct Team {
   int threads, elems;
 };
@@ -314,36 +334,52 @@ int bwd_teams(int64_t rows, int64_t cols, int64_t groups) {
   return (int)(t < 1 ? 1 : t);
 }
 
-template <typename T, int VEC, int TPR, int NC>
-void run_fwd(const LayerNormIn& in, hipStream_t stream) {
+template <typename T, int VEC, bool ONCE, int TPR, int NC>
+void run(const LayerNormIn& in, float*, hipStream_t stream) {
   const int64_t per = in.rows / in.groups;
   const dim3 grid(fwd_teams(per, in.cols, in.groups), (unsigned)in.groups);
-  layer_norm_kernel<T, VEC, TPR, NC><<<grid, TPR, 0, stream>>>(
+  layer_norm_kernel<T, VEC, ONCE, TPR, NC><<<grid, TPR, 0, stream>>>(
       static_cast<const T*>(in.x), in.ldx, per, (int)in.cols, in.weight, in.bias, in.eps,
       static_cast<T*>(in.y), in.ldy, in.mean, in.rstd);
 }
-template <typename T, int VEC, int TPR, int NC>
-void run_bwd(const LayerNormBwdIn& in, float* part, hipStream_t stream) {
+template <typename T, int VEC, bool ONCE, int TPR, int NC>
+void run(const LayerNormBwdIn& in, float* part, hipStream_t stream) {
   const int64_t per = in.rows / in.groups;
   const dim3 grid(bwd_teams(per, in.cols, in.groups), (unsigned)in.groups);
-  layer_norm_bwd_kernel<T, VEC, TPR, NC><<<grid, TPR, 0, stream>>>(
+  layer_norm_bwd_kernel<T, VEC, ONCE, TPR, NC><<<grid, TPR, 0, stream>>>(
       static_cast<const T*>(in.dy), in.lddy, static_cast<const T*>(in.x), in.ldx, in.mean, in.rstd,
       per, (int)in.cols, in.weight, static_cast<T*>(in.dx), in.lddx, part);
 }
 
-// F<T, VEC, TPR, NC>(...) for the row's type, length and alignment.
-#define SA_NORM_TEAMS(F, T, VEC, cols, BACK, ...)               \
-  do {                                                          \
-    const Team tm = team_of(cols, BACK);                        \
-    if (tm.threads == 64 && tm.elems == 8)                      \
-      F<T, VEC, 64, 8 / VEC>(__VA_ARGS__);                      \
-    else if (tm.elems <= 32 && tm.elems != 24)                  \
-      F<T, VEC, BACK ? 256 : 64, (BACK ? 8 : 32) / VEC>(__VA_ARGS__); \
-    else if (tm.elems == 24)                                    \
-      F<T, VEC, 256, 24 / VEC>(__VA_ARGS__);                    \
-    else                                                        \
-      F<T, VEC, 256, 64 / VEC>(__VA_ARGS__);                    \
-  } while (0)
+// The kernel for the row's length.
+template <typename T, int VEC, bool ONCE, typename In>
+void run_team(const In& in, float* part, hipStream_t stream) {
+  constexpr bool kBack = std::is_same<In, LayerNormBwdIn>::value;
+  const Team tm = team_of(in.cols, kBack);
+  if (in.cols <= 512)
+    run<T, VEC, ONCE, 64, 8 / VEC>(in, part, stream);
+  else if (in.cols <= 2048)
+    run<T, VEC, ONCE, kBack ? 256 : 64, (kBack ? 8 : 32) / VEC>(in, part, stream);
+  else if (tm.elems == 24)
+    run<T, VEC, ONCE, 256, 24 / VEC>(in, part, stream);
+  else
+    run<T, VEC, ONCE, 256, 64 / VEC>(in, part, stream);
+}
+// Rows of whole, aligned 16-byte pieces are moved by them (vec), others by
+// element.  More than twice what the last-level cache holds (256 MB) is kept
+// out of the caches (75,600 x 5,120 bf16: forward 321 -> 301 us, backward 460
+// -> 417); less is left in them, mostly for the call that reads the result
+// (4,680 rows: 19.5 us, kept out 22.6).
+template <typename T, typename In>
+void run_rows(const In& in, float* part, bool vec, int tensors, hipStream_t stream) {
+  const bool once = in.rows * in.cols * tensors * (int64_t)sizeof(T) > ((int64_t)512 << 20);
+  if (vec && once)
+    run_team<T, 8, true>(in, part, stream);
+  else if (vec)
+    run_team<T, 8, false>(in, part, stream);
+  else
+    run_team<T, 1, false>(in, part, stream);
+}
 
 bool whole(const void* p, int64_t ld, int elem) {  // 16-byte pieces stay aligned in every row
   return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * elem & 15) == 0;
@@ -358,19 +394,11 @@ size_t layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols, int64_t groups
 hipError_t launch_layer_norm(const LayerNormIn& in, hipStream_t stream) {
   if (in.rows == 0) return hipSuccess;
   const int elem = in.f32 ? 4 : 2;
-  // rows of whole, aligned 16-byte pieces are moved by them, others by element
   const bool vec = in.cols % 8 == 0 && whole(in.x, in.ldx, elem) && whole(in.y, in.ldy, elem);
-  if (in.f32) {
-    if (vec)
-      SA_NORM_TEAMS(run_fwd, float, 8, in.cols, false, in, stream);
-    else
-      SA_NORM_TEAMS(run_fwd, float, 1, in.cols, false, in, stream);
-  } else {
-    if (vec)
-      SA_NORM_TEAMS(run_fwd, uint16_t, 8, in.cols, false, in, stream);
-    else
-      SA_NORM_TEAMS(run_fwd, uint16_t, 1, in.cols, false, in, stream);
-  }
+  if (in.f32)
+    run_rows<float>(in, nullptr, vec, 2, stream);
+  else
+    run_rows<uint16_t>(in, nullptr, vec, 2, stream);
   return hipGetLastError();
 }
 
@@ -380,17 +408,10 @@ hipError_t launch_layer_norm_bwd(const LayerNormBwdIn& in, void* ws, hipStream_t
   if (in.rows > 0) {
     const bool vec = in.cols % 8 == 0 && whole(in.x, in.ldx, elem) &&
                      whole(in.dy, in.lddy, elem) && whole(in.dx, in.lddx, elem);
-    if (in.f32) {
-      if (vec)
-        SA_NORM_TEAMS(run_bwd, float, 8, in.cols, true, in, part, stream);
-      else
-        SA_NORM_TEAMS(run_bwd, float, 1, in.cols, true, in, part, stream);
-    } else {
-      if (vec)
-        SA_NORM_TEAMS(run_bwd, uint16_t, 8, in.cols, true, in, part, stream);
-      else
-        SA_NORM_TEAMS(run_bwd, uint16_t, 1, in.cols, true, in, part, stream);
-    }
+    if (in.f32)
+      run_rows<float>(in, part, vec, 3, stream);
+    else
+      run_rows<uint16_t>(in, part, vec, 3, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
