@@ -396,8 +396,8 @@ int sparse_attn_linear_w8a8(const uint8_t* xq, const float* sx, int64_t ldx, con
  * in the SA_FP8_K tile layout of sparse_attn_quant_fp8_tiles, those of V in its
  * SA_FP8_V layout, and one power-of-two scale each.
  *  batch       sequences B >= 1
- *  heads       query heads, a multiple of kv_heads (at most 1024 times as
- *              many): query head j shares key head j / (heads / kv_heads)
+ *  heads       query heads, a multiple of kv_heads: query head j shares key
+ *              head j / (heads / kv_heads)
  *  head_dim    must be 128
  *  tokens      T >= 0 rows of the packed tensors: row q_start[b] + i is the
  *              i-th new token of sequence b

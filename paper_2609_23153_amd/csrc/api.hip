@@ -436,7 +436,7 @@ int check_cache_desc(const sparse_attn_cache_desc* d, sa::CacheIn* c) {
   // packed rows and work items are counted in 32 bits, token positions too
   const int64_t most = (int64_t)1 << 30;
   if ((int64_t)d->tokens * d->heads > most || (int64_t)d->batch * d->heads > most / 64 ||
-      d->max_pages >= (1 << 24) || d->heads / d->kv_heads > 1024)
+      d->max_pages >= (1 << 24))
     return SA_ERR_UNSUPPORTED;
   c->B = d->batch;
   c->Hkv = d->kv_heads;

@@ -8,10 +8,12 @@
 // new token needs a larger one; then its old codes move to the new scale,
 // which is exact but for codes that become subnormal.
 //
-// One workgroup per (page that gets tokens, key head): it alone touches that
-// page's tiles, so nothing races, and it rotates the query heads that share
-// the key head.  Bound by memory: 4,680 tokens of 12 heads move 72 MB; a
-// single token is bound by the latency of its dependent loads.
+// One workgroup per page that gets tokens and key head for K, one for V, one
+// for the queries that share the key head: each tile has one writer, so nothing
+// races.  Bound by memory and, for few tokens, by the latency of dependent loads
+// (sequence, page, scale): three workgroups side by side take 4.5 us for one
+// token where one doing all took 5.8 (4,680 tokens of 12 heads, 72 MB: 19.9 us,
+// 18.8).
 #include "cache.h"
 
 namespace sa {
@@ -20,6 +22,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kGroups = kThreads / 16;  // 16 threads a row of 128 channels, 8 channels each
 constexpr int kRows = kPage / kGroups;  // rows of a page per thread
+enum { kKeys, kValues, kQueries };      // what a workgroup takes (blockIdx.y)
 
 // Smallest e >= -126 with amax <= 448 * 2^e.
 __device__ __forceinline__ int page_exponent(float amax) {
@@ -89,8 +92,8 @@ __device__ __forceinline__ uint32_t merge4(uint32_t w, uint32_t n, int k0, int l
 
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
   __shared__ __attribute__((aligned(16))) uint8_t codes[kPage * kHeadDim];  // V, by key
-  __shared__ float red[2][kThreads / kWave];
-  const int h = blockIdx.x % p.c.Hkv, item = blockIdx.x / p.c.Hkv;
+  __shared__ float red[kThreads / kWave];
+  const int h = blockIdx.x % p.c.Hkv, item = blockIdx.x / p.c.Hkv, role = blockIdx.y;
   // the sequence: its items start at q_start / 64 + 2 b, and the pages that n
   // tokens touch are at most n / 64 + 2
   Span sp;
@@ -100,126 +103,107 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
   const int page_idx = (p0 >> 6) + item - (sp.start / kPage + 2 * b);
   const int64_t base = (int64_t)page_idx * kPage;
   const int64_t end = (int64_t)sp.pos0 + sp.n;
-  if (sp.n == 0 || base >= end) return;
+  // (page_idx < 0: a decreasing q_start, which breaks the contract)
+  if (sp.n == 0 || page_idx < 0 || base >= end) return;
   const int s0 = (int)(max((int64_t)p0, base) - base), s1 = (int)(min(end, base + kPage) - base);
   const int64_t row0 = sp.start + (base - sp.pos0);  // packed row of slot 0
-  const int page = page_idx < p.c.max_pages ? p.c.pages[(int64_t)b * p.c.pages_stride + page_idx] : -1;
-  const bool held = page >= 0 && page < p.c.P;
 
   const int c8 = (threadIdx.x & 15) * 8, r0 = threadIdx.x >> 4;
-  // rows of this thread: slots r0 + 16 m
-  u32x4 kw[kRows], vw[kRows];
-#pragma unroll
-  for (int m = 0; m < kRows; ++m) {
-    const int s = r0 + kGroups * m;
-    kw[m] = vw[m] = (u32x4){0u, 0u, 0u, 0u};
-    if (s >= s0 && s < s1) {
-      kw[m] = ld16(p.k + (row0 + s) * p.k_tok + h * p.k_head + c8);
-      vw[m] = ld16(p.v + (row0 + s) * p.v_tok + h * p.v_head + c8);
-    }
-  }
-  // slot 0 starts the page anew: whatever it held before is of no sequence
-  const int64_t at = (int64_t)(held ? page : 0) * p.c.Hkv + h;
-  float* sk = p.c.sk + at;
-  float* sv = p.c.sv + at;
-  float k_was = 0.f, v_was = 0.f;
-  if (held && s0 > 0) {
-    k_was = *sk;
-    v_was = *sv;
-  }
   auto table = [&](int s) __attribute__((always_inline)) -> const float* {
     const int64_t row = p.rope_row ? (int64_t)p.rope_row[row0 + s] : base + s;
     return p.rope && row >= 0 && row < p.rope_rows ? p.rope + row * p.rope_dim : nullptr;
   };
-  // the queries that share this key head, four rows of a thread in flight
-  if (p.q) {
+  if (role == kQueries) {  // those that share this key head, four rows of a thread in flight
     const int g = p.c.g, rows = (s1 - s0) * g;
-    // i / g as a product: exact for i < 64 g, g <= 1024
-    auto over_g = [&](int i) __attribute__((always_inline)) {
-      return g == 1 ? i : (int)__umulhi((uint32_t)i, p.inv_g);
-    };
     for (int i0 = r0; i0 < rows; i0 += 4 * kGroups) {
       u32x4 w[4];
+      int s[4], hq[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int i = i0 + u * kGroups, d = over_g(i), s = s0 + d, hq = h * g + i - d * g;
-        if (i < rows) w[u] = ld16(p.q + (row0 + s) * p.q_tok + hq * p.q_head + c8);
+        const int i = i0 + u * kGroups, d = g == 1 ? i : i / g;
+        s[u] = s0 + d;
+        hq[u] = h * g + i - d * g;
+        if (i < rows) w[u] = ld16(p.q + (row0 + s[u]) * p.q_tok + hq[u] * p.q_head + c8);
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int i = i0 + u * kGroups, d = over_g(i), s = s0 + d, hq = h * g + i - d * g;
-        if (i < rows) {
+      for (int u = 0; u < 4; ++u)
+        if (i0 + u * kGroups < rows) {
           float v[8];
           widen8(v, w[u]);
-          rotate8(v, table(s), c8, p.rope_dim);
+          rotate8(v, table(s[u]), c8, p.rope_dim);
 #pragma unroll
           for (int x = 0; x < 4; ++x) w[u][x] = pack_bf16x2(v[2 * x], v[2 * x + 1]);
-          st16(p.q_out + (row0 + s) * p.qo_tok + hq * p.qo_head + c8, w[u]);
+          st16(p.q_out + (row0 + s[u]) * p.qo_tok + hq[u] * p.qo_head + c8, w[u]);
         }
+    }
+    return;
+  }
+
+  const bool is_v = role == kValues;
+  const int page = page_idx < p.c.max_pages ? p.c.pages[(int64_t)b * p.c.pages_stride + page_idx] : -1;
+  if (page < 0 || page >= p.c.P) return;
+  // rows of this thread: slots r0 + 16 m
+  const uint16_t* src = is_v ? p.v + h * p.v_head : p.k + h * p.k_head;
+  const int64_t src_tok = is_v ? p.v_tok : p.k_tok;
+  u32x4 w[kRows];
+#pragma unroll
+  for (int m = 0; m < kRows; ++m) {
+    const int s = r0 + kGroups * m;
+    w[m] = (u32x4){0u, 0u, 0u, 0u};
+    if (s >= s0 && s < s1) w[m] = ld16(src + (row0 + s) * src_tok + c8);
+  }
+  // slot 0 starts the page anew: whatever it held before is of no sequence
+  const int64_t at = (int64_t)page * p.c.Hkv + h;
+  float* scale = (is_v ? p.c.sv : p.c.sk) + at;
+  const float was = s0 > 0 ? *scale : 0.f;
+
+  float val[kRows][8];
+  float amax = 0.f;
+#pragma unroll
+  for (int m = 0; m < kRows; ++m) {
+    const int s = r0 + kGroups * m;
+    widen8(val[m], w[m]);
+    if (!is_v && s >= s0 && s < s1) rotate8(val[m], table(s), c8, p.rope_dim);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(val[m][i]));
+  }
+  amax = wave_max(amax);
+  if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = amax;
+  __syncthreads();
+  amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const int old = s0 > 0 ? max(e8m0(was) - 127, -126) : -126;
+  const int e = max(page_exponent(amax), old);
+  const bool grows = s0 > 0 && e > old;
+  const float inv = exp2_of(-e);
+  if (threadIdx.x == 0) *scale = exp2_of(e);  // (every thread read it before the barrier)
+
+  if (!is_v) {  // eight channels of a key lie side by side
+    uint8_t* kt = p.c.k8 + at * kPageBytes;
+#pragma unroll
+    for (int m = 0; m < kRows; ++m) {
+      const int s = r0 + kGroups * m;
+      const int f = 4 * (s >> 5) + 2 * (c8 >> 6) + ((c8 >> 4) & 1);
+      u32x2* to = reinterpret_cast<u32x2*>(kt + 16 * (64 * f + (s & 31) + 32 * ((c8 >> 5) & 1)) +
+                                           (c8 & 15));
+      if (s >= s0 && s < s1) {
+        *to = codes8(val[m], inv);
+      } else if (s < s0 && grows) {
+        u32x2 c = *to;
+        c[0] = rescale4(c[0], old - e);
+        c[1] = rescale4(c[1], old - e);
+        *to = c;
       }
     }
+    return;
   }
-  if (!held) return;
-
-  float kf[kRows][8];
-  float ka = 0.f, va = 0.f;
-#pragma unroll
-  for (int m = 0; m < kRows; ++m) {
-    const int s = r0 + kGroups * m;
-    widen8(kf[m], kw[m]);
-    if (s >= s0 && s < s1) rotate8(kf[m], table(s), c8, p.rope_dim);
-    float t[8];
-    widen8(t, vw[m]);
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      ka = fmaxf(ka, fabsf(kf[m][x]));
-      va = fmaxf(va, fabsf(t[x]));
-    }
-  }
-  ka = wave_max(ka);
-  va = wave_max(va);
-  if ((threadIdx.x & (kWave - 1)) == 0) {
-    red[0][threadIdx.x / kWave] = ka;
-    red[1][threadIdx.x / kWave] = va;
-  }
-  const int k_old = s0 > 0 ? e8m0(k_was) - 127 : -126, v_old = s0 > 0 ? e8m0(v_was) - 127 : -126;
-  __syncthreads();
-  ka = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  va = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
-  const int ke = max(page_exponent(ka), max(k_old, -126));
-  const int ve = max(page_exponent(va), max(v_old, -126));
-  const bool k_grows = s0 > 0 && ke > k_old, v_grows = s0 > 0 && ve > v_old;
-
-  uint8_t* kt = p.c.k8 + at * kPageBytes;
   uint8_t* vt = p.c.v8 + at * kPageBytes;
-  // K: eight channels of a key lie side by side
-  const float kinv = exp2_of(-ke), vinv = exp2_of(-ve);
 #pragma unroll
-  for (int m = 0; m < kRows; ++m) {
-    const int s = r0 + kGroups * m;
-    const int f = 4 * (s >> 5) + 2 * (c8 >> 6) + ((c8 >> 4) & 1);
-    u32x2* to = reinterpret_cast<u32x2*>(kt + 16 * (64 * f + (s & 31) + 32 * ((c8 >> 5) & 1)) +
-                                         (c8 & 15));
-    if (s >= s0 && s < s1) {
-      *to = codes8(kf[m], kinv);
-    } else if (s < s0 && k_grows) {
-      u32x2 w = *to;
-      w[0] = rescale4(w[0], k_old - ke);
-      w[1] = rescale4(w[1], k_old - ke);
-      *to = w;
-    }
-    float t[8];
-    widen8(t, vw[m]);
-    *reinterpret_cast<u32x2*>(codes + s * kHeadDim + c8) = codes8(t, vinv);
-  }
+  for (int m = 0; m < kRows; ++m)
+    *reinterpret_cast<u32x2*>(codes + (r0 + kGroups * m) * kHeadDim + c8) = codes8(val[m], inv);
   __syncthreads();
-  if (threadIdx.x == 0) {
-    *sk = exp2_of(ke);
-    *sv = exp2_of(ve);
-  }
   // V: 16 keys of a channel lie side by side, four in a row.  A thread turns
   // four channels of the 16 keys 32 hf + 8 q4 + 4 g + x: 4 x 4 bytes at a time.
-  if (s1 - s0 <= 8 && !v_grows) {  // a few new keys: byte by byte, a channel a thread
+  if (s1 - s0 <= 8 && !grows) {  // a few new keys: byte by byte, a channel a thread
     const int ch = threadIdx.x & 127;
     for (int s = s0 + (threadIdx.x >> 7); s < s1; s += 2)
       vt[16 * (64 * (2 * (ch >> 5) + (s >> 5)) + (ch & 31) + 32 * ((s >> 2) & 1)) +
@@ -257,12 +241,12 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           const int k0 = k_first + 8 * q4;
-          const bool any = k0 < s1 && k0 + 4 > s0, old = v_grows && k0 < s0;
+          const bool any = k0 < s1 && k0 + 4 > s0, again = grows && k0 < s0;
           if (k0 >= s0 && k0 + 4 <= s1) {
             to[q4] = n[j][q4];
-          } else if (old) {
-            const uint32_t w = to[q4];
-            to[q4] = merge4(merge4(w, rescale4(w, v_old - ve), k0, 0, s0), n[j][q4], k0, s0, s1);
+          } else if (again) {
+            const uint32_t c = to[q4];
+            to[q4] = merge4(merge4(c, rescale4(c, old - e), k0, 0, s0), n[j][q4], k0, s0, s1);
           } else if (any) {  // slots past the new ones are left as they are
 #pragma unroll
             for (int x = 0; x < 4; ++x)
@@ -282,9 +266,7 @@ int64_t cache_append_items(const CacheIn& c) { return (int64_t)c.T / kPage + 2 *
 hipError_t launch_cache_append(const AppendIn& in, hipStream_t stream) {
   if (in.c.T == 0) return hipSuccess;
   const int64_t n = cache_append_items(in.c) * in.c.Hkv;
-  AppendIn a = in;
-  a.inv_g = 0xffffffffu / (uint32_t)a.c.g + 1u;  // ceil(2^32 / g), g > 1
-  cache_append_kernel<<<(unsigned)n, kThreads, 0, stream>>>(a);
+  cache_append_kernel<<<dim3((unsigned)n, in.q ? 3 : 2), kThreads, 0, stream>>>(in);
   return hipGetLastError();
 }
 

@@ -76,7 +76,7 @@ __device__ __forceinline__ bool find_tile(const CacheIn& c, int w, Tile* t) {
   if (t->b < 0) return false;
   t->rows = t->sp.n * c.g;
   const int64_t row0 = (int64_t)(w - first(t->sp.start, t->b)) * R;
-  if (row0 >= t->rows) return false;
+  if (row0 < 0 || row0 >= t->rows) return false;  // (< 0: a decreasing q_start)
   t->row0 = (int)row0;
   tile_range<R>(c, t);
   return true;
@@ -690,7 +690,7 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
   const int tok = (int)(row / p.H), head = (int)(row - (int64_t)tok * p.H);
   Tile t;
   t.b = find_sequence(p.c, tok, [](int s, int) { return s; }, &t.sp);
-  if (t.b < 0 || tok - t.sp.start >= t.sp.n) return;
+  if (t.b < 0 || tok < t.sp.start || tok - t.sp.start >= t.sp.n) return;
   t.rows = t.sp.n * p.c.g;
   t.row0 = ((tok - t.sp.start) * p.c.g + head % p.c.g) / R * R;
   tile_range<R>(p.c, &t);

@@ -181,7 +181,6 @@ struct AppendIn {
   const int32_t* rope_row; // [T] rows of the table, or null: positions
   int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head, qo_tok, qo_head, rope_rows;
   int rope_dim;
-  uint32_t inv_g;          // set by the launcher
 };
 int64_t cache_append_items(const CacheIn& c);  // (page, sequence) work items at most
 hipError_t launch_cache_append(const AppendIn& in, hipStream_t stream);

@@ -238,6 +238,46 @@ def test_out_of_contract_lengths_stay_in_bounds():
             compare(o, lse, q, (k8, sk, v8, sv), pages, start, lengths, 1, 0, what=f"{start} {lengths}")
 
 
+def test_decreasing_starts_stay_in_bounds():
+    # q_start has to be non-decreasing; where it is not, results are undefined,
+    # but nothing outside the tensors is touched
+    lengths = [700, 64, 300, 80]
+    for most in (11, 40):                                # few rows, many rows
+        k8, sk, v8, sv, pages = make_cache(lengths, 2, 18, most=most)
+        for n, start in ((40, [0, 30, 10, 35, 40]), (4000, [3900, 100, 2000, 50, 4000])):
+            q = queries(n, 4, 19)
+            pool = [t.clone() for t in (k8, sk, v8, sv)]
+            kv = queries(n, 2, 20)
+            sa.sparse_attn_cache_append(kv, kv, *pool, ints(pages), ints(start), ints(lengths), q=q)
+            sa.sparse_attn_fwd_cache(q, k8, sk, v8, sv, ints(pages), ints(start), ints(lengths))
+    torch.cuda.synchronize()
+
+
+def test_pool_beyond_32_bit_offsets():
+    # the same pages at the end of a pool of 4.9 GB a tensor
+    lengths, kv = [1000, 70], 8
+    k8, sk, v8, sv, pages = make_cache(lengths, kv, 21)
+    P, far = 75000, 75000 - len(k8)
+    big = [torch.zeros(P, kv, 8192, dtype=torch.uint8, device=DEV), torch.ones(P, kv, device=DEV),
+           torch.zeros(P, kv, 8192, dtype=torch.uint8, device=DEV), torch.ones(P, kv, device=DEV)]
+    for t, x in zip(big, (k8, sk, v8, sv)):
+        t[far:] = x
+    moved = np.where(pages >= 0, pages + far, -1)
+    for new in ([1, 1], [200, 33]):
+        start = np.concatenate([[0], np.cumsum(new)])
+        q, x = queries(sum(new), 16, 22), queries(sum(new), kv, 23)
+        small = [k8.clone(), sk.clone(), v8.clone(), sv.clone()]
+        sa.sparse_attn_cache_append(x, x, *small, ints(pages), ints(start), ints(lengths))
+        sa.sparse_attn_cache_append(x, x, *big, ints(moved), ints(start), ints(lengths))
+        for a, b in zip(big, small):
+            assert torch.equal(a[far:], b)
+        want = sa.sparse_attn_fwd_cache(q, *small, ints(pages), ints(start), ints(lengths), causal=(1, 0))
+        got = sa.sparse_attn_fwd_cache(q, *big, ints(moved), ints(start), ints(lengths), causal=(1, 0))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        k8, sk, v8, sv = small
+    assert not bool(big[0][:far].any()) and not bool(big[2][:far].any())
+
+
 def test_no_tokens():
     k8, sk, v8, sv, pages = make_cache([64], 1, 14)
     q = queries(0, 2, 15)

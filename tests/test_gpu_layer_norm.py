@@ -151,6 +151,30 @@ def test_in_place_equals_out_of_place_and_repeats_bit_for_bit():
     assert torch.equal(only, dx) and none is None and nope is None
 
 
+def test_larger_than_the_caches_equals_its_parts():
+    # rows that are kept out of the caches (over 512 MB) against the same rows a
+    # part at a time; fp32 and bf16, whole and with a padded row
+    for dtype, rows, cols, pad in ((torch.bfloat16, 14000, 10240, 0), (torch.float32, 9001, 8200, 8)):
+        g = torch.Generator(device=DEV).manual_seed(rows)
+        rnd = lambda *s: torch.randn(*s, generator=g, device=DEV)
+        x, dy = (rnd(rows, cols + pad).to(dtype)[:, :cols] for _ in range(2))
+        w, b = 1 + 0.3 * rnd(cols), rnd(cols)
+        y, mean, rstd = sa.sparse_attn_layer_norm(x, w, b)
+        dx, dw, db = sa.sparse_attn_layer_norm_bwd(dy, x, mean, rstd, w)
+        sw, sb = torch.zeros(2, cols, dtype=torch.float64, device=DEV)
+        for r in range(0, rows, 1500):
+            part = slice(r, r + 1500)
+            py, pm, pr = sa.sparse_attn_layer_norm(x[part], w, b)
+            assert torch.equal(py, y[part]) and torch.equal(pm, mean[part]) and torch.equal(pr, rstd[part])
+            pdx, pdw, pdb = sa.sparse_attn_layer_norm_bwd(dy[part], x[part], pm, pr, w)
+            assert torch.equal(pdx, dx[part])
+            sw += pdw
+            sb += pdb
+        # sums of `rows` terms of size about 1 (dy xh): two orders of fp32 additions
+        # differ by at most 2 F32 of the sum of magnitudes, below 2 F32 rows here
+        assert (dw - sw).abs().max() <= 2 * F32 * rows and (db - sb).abs().max() <= 2 * F32 * rows
+
+
 def test_captured_and_replayed():
     x, dy, w, b, _ = make(300, 2056, torch.bfloat16, 1)
     step = lambda: (lambda y, m, r: (y,) + sa.sparse_attn_layer_norm_bwd(dy, x, m, r, w))(
