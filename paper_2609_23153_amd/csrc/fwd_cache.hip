@@ -13,9 +13,14 @@
 // share a key head are rows side by side).  Two kernels share that step:
 //   few rows   (<= 32 a sequence on average): bound by the cache's bytes; the
 //              waves of a workgroup take pages in turn, straight into
-//              registers, and merge their softmax states through LDS
-//   many rows  bound by the matrix cores; four waves of 32 rows share every
-//              page through LDS, copied two pages ahead
+//              registers, the next page's while one is worked on, and merge
+//              their softmax states through LDS.  One token over 524,288 (40
+//              heads on 8): 170 us, 6.3 TB/s of the cache's bytes
+//   many rows  bound by the matrix cores and the vector work beside them; four
+//              waves of 32 rows share every page through LDS, copied up to
+//              three pages ahead.  4,680 tokens over 32,760 (12 heads): 0.94 ms,
+//              1,000 TFLOP/s (a large bf16 library product: 1,380), matrix
+//              cores busy 43% of the cycles, vector units 57%, at 2.05 GHz
 // Long key ranges are cut over workgroups when there are few rows: partial
 // sums go to the workspace and a second kernel joins them in a fixed order.
 #include <type_traits>
@@ -184,10 +189,11 @@ __device__ __forceinline__ f32x16 scores(const Wave& w, const i32x8& k0, const i
   return SA_MFMA(k1, w.qh[1], s, sk, w.qh_code);
 }
 
-// Scores of keys outside a row's range (page's first key: start) become -inf.
-__device__ __forceinline__ void mask_scores(const Wave& w, int start, f32x16 (&s)[2]) {
+// Scores of keys outside a row's range, or at or past `keys`, become -inf
+// (page's first key: start).
+__device__ __forceinline__ void mask_scores(const Wave& w, int start, int keys, f32x16 (&s)[2]) {
   const int g = (threadIdx.x >> 5) & 1;
-  const int hi = w.hi - start - 4 * g, lo = w.lo - start - 4 * g;
+  const int hi = min(w.hi, keys) - start - 4 * g, lo = w.lo - start - 4 * g;
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
@@ -347,12 +353,11 @@ __device__ __forceinline__ void store_sums(const Params& p, const Wave& w, float
 // ---- few rows ---------------------------------------------------------------
 constexpr int kFewRows = 32;
 
-__device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* tile) {
-  const int lane = threadIdx.x & (kWave - 1);
+__device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* tile, int at) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const u32x4 lo = ld16_once(tile + 2048 * i + 16 * lane);
-    const u32x4 hi = ld16_once(tile + 2048 * i + 1024 + 16 * lane);
+    const u32x4 lo = ld16_once(tile + 2048 * i + at);
+    const u32x4 hi = ld16_once(tile + 2048 * i + 1024 + at);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       f[i][x] = (int)lo[x];
@@ -376,37 +381,54 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
   const int to = (int)((int64_t)t.pages * (split + 1) / parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Wave w;
-  wave_init(p, t, h, t.row0, &w);
   const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
 
-  // pages from + wave + 4 i, 64 of them known at a time
+  // pages from + wave + 4 i, 64 of them known at a time; K of the next one loads
+  // once S has been computed, V once it has been multiplied, into the same
+  // registers (where there is no page, page 0's tiles, of which nothing is used)
   const int mine = to > from + wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
-  PageInfo info;
-  for (int i = 0; i < mine; ++i) {
-    const int n = from + wave + kWaves * i;
-    if ((i & (kWave - 1)) == 0) info = page_info(p.c, table, h, n, kWaves, to);
-    const int page = __builtin_amdgcn_readlane(info.page, i & (kWave - 1));
-    if (page < 0) continue;
-    const int64_t at = ((int64_t)page * p.c.Hkv + h) * kPageBytes;
+  auto tile_at = [&](int page) __attribute__((always_inline)) {
+    return ((int64_t)max(page, 0) * p.c.Hkv + h) * kPageBytes;
+  };
+  if (mine > 0) {
+    PageInfo info = page_info(p.c, table, h, from + wave, kWaves, to);
+    int page = __builtin_amdgcn_readlane(info.page, 0);
     i32x8 kf[4], vf[4];
-    load_fragments(kf, p.c.k8 + at);
-    load_fragments(vf, p.c.v8 + at);
-    // (the scales may still be on their way when the tiles are asked for)
-    __builtin_amdgcn_sched_barrier(0);
-    const int scales = __builtin_amdgcn_readlane(info.scales, i & (kWave - 1));
-    const int sk = scales & 0xff, sv = scales >> 8, start = (t.page_lo + n) * kPage;
-    f32x16 s[2];
-    s[0] = scores(w, kf[0], kf[1], sk);
-    s[1] = scores(w, kf[2], kf[3], sk);
-    if (needs_mask(w, start)) mask_scores(w, start, s);
-    raise_max(w, page_max(s), p.scale_log2);
-    const float off = exp_offset(w);
-    i32x8 ph;
-    numerators(w, p.scale_log2, off, s[0], ph, 0);
-    numerators(w, p.scale_log2, off, s[1], ph, 4);
-    if (start + kPage > t.sp.keys) clear_tail(vf, start, t.sp.keys);
-    add_values(w, vf, ph, sv, 0);
-    add_values(w, vf, rests(s, ph), sv, kRestP);
+    const int mine16 = 16 * (threadIdx.x & (kWave - 1));  // this lane's bytes of a fragment
+    load_fragments(kf, p.c.k8 + tile_at(page), mine16);
+    load_fragments(vf, p.c.v8 + tile_at(page), mine16);
+    wave_init(p, t, h, t.row0, &w);
+    for (int i = 0; i < mine; ++i) {
+      const int n = from + wave + kWaves * i, start = (t.page_lo + n) * kPage;
+      const int scales = __builtin_amdgcn_readlane(info.scales, i & (kWave - 1));
+      const int sk = scales & 0xff, sv = scales >> 8, j = (i + 1) & (kWave - 1);
+      if (j == 0 && i + 1 < mine) info = page_info(p.c, table, h, n + kWaves, kWaves, to);
+      // after the last page every lane asks for the same few bytes again, which
+      // costs less than a branch here
+      const bool more = i + 1 < mine;
+      const int next = more ? __builtin_amdgcn_readlane(info.page, j) : page;
+      const int64_t at = tile_at(next);
+      const int lane16 = more ? mine16 : 0;
+      f32x16 s[2];
+      s[0] = scores(w, kf[0], kf[1], sk);
+      s[1] = scores(w, kf[2], kf[3], sk);
+      load_fragments(kf, p.c.k8 + at, lane16);
+      const int keys = page >= 0 ? t.sp.keys : start;  // none of a missing page
+      if (start + kPage > keys || needs_mask(w, start)) mask_scores(w, start, keys, s);
+      raise_max(w, page_max(s), p.scale_log2);
+      const float off = exp_offset(w);
+      i32x8 ph;
+      numerators(w, p.scale_log2, off, s[0], ph, 0);
+      numerators(w, p.scale_log2, off, s[1], ph, 4);
+      const i32x8 pl = rests(s, ph);
+      if (start + kPage > keys) clear_tail(vf, start, keys);
+      add_values(w, vf, ph, sv, 0);
+      add_values(w, vf, pl, sv, kRestP);
+      load_fragments(vf, p.c.v8 + at, lane16);
+      page = next;
+    }
+  } else {
+    wave_init(p, t, h, t.row0, &w);
   }
 
   // join the waves: wave i takes channels 32 i .. 32 i + 31
@@ -572,7 +594,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
 #pragma unroll
           for (int rt = 0; rt < 2; ++rt)
             s[rt] = scores(w, lds_fragment(tile[0], 2 * rt), lds_fragment(tile[0], 2 * rt + 1), pg0.sk);
-          if (needs_mask(w, start)) mask_scores(w, start, s);
+          if (needs_mask(w, start)) mask_scores(w, start, t.sp.keys, s);
           raise_max(w, page_max(s), p.scale_log2);
           const float off = exp_offset(w);
           i32x8 ph, f[4];
@@ -721,6 +743,10 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
 // the cache's bytes.  A part is given at least one page a wave where there are
 // not enough workgroups for every CU, four where there are (its start and end
 // cost about as much as two pages).
+// Short tables are not cut: one token over 24 pages of 12 heads takes 12.7 us in
+// a stream of calls and 32 alone whole, 15.6 and 30 in parts; over 32 pages 15.1
+// and 34, in parts 15.8 and 30.
+constexpr int kWhole = 24;  // pages
 struct Plan {
   bool few;
   int64_t tiles;
@@ -745,6 +771,7 @@ Plan plan_of(const CacheIn& c) {
     s = have >= kSlots / 2 ? 1 : kSlots / have;
   }
   if (s > c.max_pages / pl.least) s = c.max_pages / pl.least;
+  if (c.max_pages <= kWhole) s = 1;
   pl.splits = (int)(s < 1 ? 1 : s > kWave ? kWave : s);
   return pl;
 }
