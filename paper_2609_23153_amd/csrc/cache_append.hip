@@ -22,6 +22,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kGroups = kThreads / 16;  // 16 threads a row of 128 channels, 8 channels each
 constexpr int kRows = kPage / kGroups;  // rows of a page per thread
+constexpr int kRowBytes = kHeadDim + 16;    // of a key's codes in LDS: its 16-byte pieces spread over the banks
 enum { kKeys, kValues, kQueries };      // what a workgroup takes (blockIdx.y)
 
 // Smallest e >= -126 with amax <= 448 * 2^e.
@@ -91,7 +92,7 @@ __device__ __forceinline__ uint32_t merge4(uint32_t w, uint32_t n, int k0, int l
 }
 
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
-  __shared__ __attribute__((aligned(16))) uint8_t codes[kPage * kHeadDim];  // V, by key
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kPage * kRowBytes];  // by key
   __shared__ float red[kThreads / kWave];
   const int h = blockIdx.x % p.c.Hkv, item = blockIdx.x / p.c.Hkv, role = blockIdx.y;
   // the sequence: its items start at q_start / 64 + 2 b, and the pages that n
@@ -177,46 +178,45 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
   const float inv = exp2_of(-e);
   if (threadIdx.x == 0) *scale = exp2_of(e);  // (every thread read it before the barrier)
 
-  if (!is_v) {  // eight channels of a key lie side by side
+#pragma unroll
+  for (int m = 0; m < kRows; ++m)
+    *reinterpret_cast<u32x2*>(codes + (r0 + kGroups * m) * kRowBytes + c8) = codes8(val[m], inv);
+  __syncthreads();
+  if (!is_v) {  // K: 16 channels of a key lie side by side, then the next key's
     uint8_t* kt = p.c.k8 + at * kPageBytes;
 #pragma unroll
-    for (int m = 0; m < kRows; ++m) {
-      const int s = r0 + kGroups * m;
-      const int f = 4 * (s >> 5) + 2 * (c8 >> 6) + ((c8 >> 4) & 1);
-      u32x2* to = reinterpret_cast<u32x2*>(kt + 16 * (64 * f + (s & 31) + 32 * ((c8 >> 5) & 1)) +
-                                           (c8 & 15));
+    for (int j = 0; j < kPageBytes / 16 / kThreads; ++j) {
+      const int c = threadIdx.x + kThreads * j, f = c >> 6;
+      const int s = 32 * (f >> 2) + (c & 31);
+      const int ch = 64 * ((f >> 1) & 1) + 32 * ((c >> 5) & 1) + 16 * (f & 1);
       if (s >= s0 && s < s1) {
-        *to = codes8(val[m], inv);
+        st16(kt + 16 * c, ld16(codes + s * kRowBytes + ch));
       } else if (s < s0 && grows) {
-        u32x2 c = *to;
-        c[0] = rescale4(c[0], old - e);
-        c[1] = rescale4(c[1], old - e);
-        *to = c;
+        u32x4 o = ld16(kt + 16 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = rescale4(o[i], old - e);
+        st16(kt + 16 * c, o);
       }
     }
     return;
   }
   uint8_t* vt = p.c.v8 + at * kPageBytes;
-#pragma unroll
-  for (int m = 0; m < kRows; ++m)
-    *reinterpret_cast<u32x2*>(codes + (r0 + kGroups * m) * kHeadDim + c8) = codes8(val[m], inv);
-  __syncthreads();
   // V: 16 keys of a channel lie side by side, four in a row.  A thread turns
   // four channels of the 16 keys 32 hf + 8 q4 + 4 g + x: 4 x 4 bytes at a time.
   if (s1 - s0 <= 8 && !grows) {  // a few new keys: byte by byte, a channel a thread
     const int ch = threadIdx.x & 127;
     for (int s = s0 + (threadIdx.x >> 7); s < s1; s += 2)
       vt[16 * (64 * (2 * (ch >> 5) + (s >> 5)) + (ch & 31) + 32 * ((s >> 2) & 1)) +
-         4 * ((s >> 3) & 3) + (s & 3)] = codes[s * kHeadDim + ch];
+         4 * ((s >> 3) & 3) + (s & 3)] = codes[s * kRowBytes + ch];
   } else if (threadIdx.x < 128) {
     const int ch = 4 * (threadIdx.x & 31), g = (threadIdx.x >> 5) & 1, hf = threadIdx.x >> 6;
     uint32_t n[4][4];  // [channel][q4]: keys x of a channel as bytes
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
-      const uint8_t* from = codes + (32 * hf + 8 * q4 + 4 * g) * kHeadDim + ch;
+      const uint8_t* from = codes + (32 * hf + 8 * q4 + 4 * g) * kRowBytes + ch;
       uint32_t r[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) r[x] = *reinterpret_cast<const uint32_t*>(from + x * kHeadDim);
+      for (int x = 0; x < 4; ++x) r[x] = *reinterpret_cast<const uint32_t*>(from + x * kRowBytes);
       // v_perm_b32: byte selectors 0-3 take the second operand's bytes, 4-7 the first's
       const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u);  // k0c0 k1c0 k0c1 k1c1
       const uint32_t b = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u);
