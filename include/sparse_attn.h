@@ -472,9 +472,9 @@ size_t sparse_attn_fwd_cache_workspace_size(const sparse_attn_cache_desc* desc);
  * of pages outside the pool:
  *   o_t = sum_u softmax_u(tau q_t.k_u) v_u,  lse_t = log sum_u exp(tau q_t.k_u)
  * on the dequantised keys and values; a query that sees no key gets o = 0 and
- * lse = -inf.  Products accumulate in fp32; the queries enter exactly (but for
- * 2^-23 of their row's largest element), the probabilities rounded to 8
- * significant bits, the row sums unrounded.  Cached tokens that some query of
+ * lse = -inf.  Products accumulate in fp32; queries, keys and values enter
+ * exactly, the probabilities rounded to 8 significant bits, the row sums
+ * unrounded.  Cached tokens that some query of
  * the call sees must be finite; the slots behind the last token may hold
  * anything.  Call sparse_attn_cache_append for the new tokens first.
  *  q, o     bf16 [T][heads][128] via q_stride, o_stride; o must not overlap q

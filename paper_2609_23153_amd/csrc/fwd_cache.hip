@@ -1,13 +1,14 @@
 // Attention of the newest tokens over the paged e4m3 cache, gfx950.
 //
-// Exact softmax attention of bf16 queries over dequantised keys and values:
-// both products run on the fp8 matrix cores, K and V straight from the cache
-// in operand order, their scales entering as E8M0 operands.  The other operand
-// is split in two e4m3 terms, x = h + l with l the rounded rest: four
-// significant bits each, so h + l holds a bf16 query exactly (but for 2^-23 of
-// its row's largest element) and a probability to 8 bits, and two fp8 products
-// cost what one bf16 product would, without converting K or V.  Row sums take
-// the unrounded probabilities in fp32.
+// Exact softmax attention of bf16 queries over dequantised keys and values.
+// Scores are products of the queries with K widened to bf16, which is exact
+// (four significant bits, a power-of-two scale), with fp32 sums: the fp8 matrix
+// instructions drop low bits of small products, up to 1.3e-5 of a sum's
+// magnitudes, which would be the error of lse.  P . V runs on the fp8 matrix
+// cores, V straight from the cache in operand order, its scale as an E8M0
+// operand; P is split in two e4m3 terms, p = h + l with l the rounded rest: eight
+// significant bits, as in bf16, at the cost of one bf16 product and without
+// converting V.  Row sums take the unrounded probabilities in fp32.
 //
 // A wave serves 32 rows (a row: one query head of one token; the heads that
 // share a key head are rows side by side).  Two kernels share that step:
@@ -38,9 +39,9 @@ constexpr float kLn2 = 0.69314718055994531f;
 // before the accumulators are rescaled (448 is the largest e4m3 value).
 constexpr float kLogP = 6.f;
 constexpr float kLazy = 2.f;
-// The rests are scaled up: |x - h| is at most half a step, 16 (x <= 448), so
-// 16 (x - h) <= 256 for queries; 8 (x <= 256) and 32 (x - h) <= 256 for P.
-constexpr int kRestQ = 4, kRestP = 5;  // log2 of those factors
+// The rests are scaled up: |x - h| is at most half a step, 8 (x <= 256), and
+// 32 (x - h) <= 256.
+constexpr int kRestP = 5;              // log2 of that factor
 constexpr int kOne = 127;              // E8M0 code of 1
 
 struct Params {
@@ -94,8 +95,7 @@ __device__ __forceinline__ int parts_of(int pages, int splits, int least) {
 
 // ---- one wave's rows --------------------------------------------------------
 struct Wave {
-  i32x8 qh[2], ql[2];   // queries, B operands of K . Q^T
-  int qh_code, ql_code;
+  bf16x8 q[8];          // queries, B operands of K . Q^T: channels 64 (i / 4) + 32 g + 8 (i % 4)
   f32x16 acc[4];        // O^T: channels 32 dt + 8 (r / 4) + 4 g + r % 4 of row l32
   float m, l;           // running maximum (log2 units), the lane's row sum
   int lo, hi;           // keys that the lane's row sees
@@ -138,38 +138,9 @@ __device__ __forceinline__ void wave_init(const Params& p, const Tile& t, int h,
   w->all_hi = __builtin_amdgcn_readfirstlane(w->hi);
   w->all_lo = __builtin_amdgcn_readlane(w->lo, 31);
   const uint16_t* q = p.q + tok * p.q_tok + head * p.q_head + 32 * g;
-  u32x4 x[2][4];
-  uint32_t amax = 0;
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[ks][j] = ld16(q + 64 * ks + 8 * j);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        amax = max(amax, max(x[ks][j][e] & 0x7fffu, (x[ks][j][e] >> 16) & 0x7fffu));
-    }
-  // a power of two that brings the row's largest element into (224, 448]
-  const float big = pair_max32(__uint_as_float(amax << 16));
-  int e = -100;
-  if (big > 0.f) {
-    int ex;
-    const float fr = frexpf(big, &ex);
-    e = max(ex - 9 + (fr > 0.875f ? 1 : 0), -100);
-  }
-  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-  w->qh_code = kOne + e;
-  w->ql_code = kOne + e - kRestQ;
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t a = x[ks][j / 2][2 * (j & 1)], b = x[ks][j / 2][2 * (j & 1) + 1];
-      const float v[4] = {bf16_lo(a) * inv, bf16_hi(a) * inv, bf16_lo(b) * inv, bf16_hi(b) * inv};
-      const int hi = cvt4(v[0], v[1], v[2], v[3]);
-      w->qh[ks][j] = hi;
-      w->ql[ks][j] = rest4(v[0], v[1], v[2], v[3], hi, (float)(1 << kRestQ));
-    }
+  for (int i = 0; i < 8; ++i)
+    w->q[i] = __builtin_bit_cast(bf16x8, ld16(q + 64 * (i >> 2) + 8 * (i & 3)));
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -181,12 +152,30 @@ __device__ __forceinline__ void wave_init(const Params& p, const Tile& t, int h,
 #define SA_MFMA(a, b, c, ca, cb) \
   __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, ca, 0, cb)
 
-// S^T of 32 keys of a page x 32 rows: K fragments k0, k1 (channels 0-63, 64-127).
-__device__ __forceinline__ f32x16 scores(const Wave& w, const i32x8& k0, const i32x8& k1, int sk) {
-  f32x16 s = SA_MFMA(k0, w.ql[0], (f32x16){}, sk, w.ql_code);
-  s = SA_MFMA(k1, w.ql[1], s, sk, w.ql_code);
-  s = SA_MFMA(k0, w.qh[0], s, sk, w.qh_code);
-  return SA_MFMA(k1, w.qh[1], s, sk, w.qh_code);
+// Eight channels of K, of the lane's key, as bf16: codes in two words times the
+// page's scale (exact).
+__device__ __forceinline__ bf16x8 widen_k(uint32_t a, uint32_t b, float scale) {
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true));
+  return __builtin_bit_cast(bf16x8, o);
+}
+// The scale whose E8M0 code is given.
+__device__ __forceinline__ float scale_of(int code) { return __uint_as_float((uint32_t)code << 23); }
+
+// S^T of 32 keys of a page x 32 rows from the fragments of their codes,
+// channels 0-63 and 64-127.
+__device__ __forceinline__ f32x16 scores(const Wave& w, const i32x8& k0, const i32x8& k1, float scale) {
+  f32x16 s = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const i32x8& k = i < 4 ? k0 : k1;
+    const int j = 2 * (i & 3);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_k(k[j], k[j + 1], scale), w.q[i], s, 0, 0, 0);
+  }
+  return s;
 }
 
 // Scores of keys outside a row's range, or at or past `keys`, become -inf
@@ -284,12 +273,11 @@ struct PageInfo {
 struct PageAt {  // one of them, uniform
   int page, sk, sv;
 };
-// Lane i takes table entry first + stride * i, if below `end`.
-__device__ __forceinline__ PageInfo page_info(const CacheIn& c, const int32_t* table, int h, int first,
-                                              int stride, int end) {
-  const int64_t i = first + (int64_t)stride * (threadIdx.x & (kWave - 1));
+// The lane's page is table entry i, if there is one.
+__device__ __forceinline__ PageInfo page_info(const CacheIn& c, const int32_t* table, int h, int64_t i,
+                                              bool there) {
   PageInfo f{-1, kOne | (kOne << 8)};
-  if (i < end) {
+  if (there) {
     const int page = table[i];
     if (page >= 0 && page < c.P) {
       const int64_t at = (int64_t)page * c.Hkv + h;
@@ -298,6 +286,12 @@ __device__ __forceinline__ PageInfo page_info(const CacheIn& c, const int32_t* t
     }
   }
   return f;
+}
+// Lane i takes table entry first + stride * i, if below `end`.
+__device__ __forceinline__ PageInfo page_info(const CacheIn& c, const int32_t* table, int h, int first,
+                                              int stride, int end) {
+  const int64_t i = first + (int64_t)stride * (threadIdx.x & (kWave - 1));
+  return page_info(c, table, h, i, i < end);
 }
 __device__ __forceinline__ PageAt page_at(const PageInfo& f, int lane) {
   const int s = __builtin_amdgcn_readlane(f.scales, lane);
@@ -401,7 +395,8 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
     for (int i = 0; i < mine; ++i) {
       const int n = from + wave + kWaves * i, start = (t.page_lo + n) * kPage;
       const int scales = __builtin_amdgcn_readlane(info.scales, i & (kWave - 1));
-      const int sk = scales & 0xff, sv = scales >> 8, j = (i + 1) & (kWave - 1);
+      const float sk = scale_of(scales & 0xff);
+      const int sv = scales >> 8, j = (i + 1) & (kWave - 1);
       if (j == 0 && i + 1 < mine) info = page_info(p.c, table, h, n + kWaves, kWaves, to);
       // after the last page every lane asks for the same few bytes again, which
       // costs less than a branch here
@@ -481,18 +476,32 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
 }
 
 // ---- many rows ----------------------------------------------------------------
-// Pages are copied to LDS up to three ahead, shared by the four waves.  Most
-// pages are seen whole by every row of the tile: they form one range, and go
-// through a loop without masks or branches whose steps hold matrix work and
-// independent vector work side by side: S(n + 1) beside the numerators of page
-// n, the products of P(n)'s leading terms beside their rests, those of the rests
-// beside the maxima of S(n + 1).  (Spelling the order of the two out, with
-// scheduling groups of 14 vector instructions a product, made it 3% slower.)
-// The pages before and after that range (causal borders, the sequence's last
-// page) come first, one by one.
+// The four waves share every page through LDS: K widened to bf16 by a quarter
+// each, V as it is.  Most pages are seen whole by every row of the tile: they
+// form one range, and go through a loop without masks or branches whose steps
+// hold matrix work and independent vector work side by side: S(n + 1) beside the
+// numerators of page n, the products of P(n)'s leading terms beside their rests,
+// those of the rests beside the maxima of S(n + 1).  (Spelling the order of the
+// two out, with scheduling groups of 14 vector instructions a product, made it
+// 3% slower.)  The pages before and after that range (causal borders, the
+// sequence's last page) come first, one by one.
 constexpr int kManyRows = kWaves * kWaveRows;
-constexpr int kStages = 4;
 
+struct ManyShared {
+  uint8_t k[2][2 * kPageBytes];  // bf16: 1 KB for each (32 keys, 16 channels) in operand order
+  uint8_t v[2][kPageBytes];
+};
+
+// S^T of 32 keys (rt: which) of a page in LDS.
+__device__ __forceinline__ f32x16 lds_scores(const Wave& w, const uint8_t* k, int rt) {
+  f32x16 s = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        __builtin_bit_cast(bf16x8, ld16(k + 1024 * (8 * rt + i) + 16 * (threadIdx.x & (kWave - 1)))),
+        w.q[i], s, 0, 0, 0);
+  return s;
+}
 __device__ __forceinline__ i32x8 lds_fragment(const uint8_t* tile, int i) {
   const uint8_t* s = tile + 2048 * i + 16 * (threadIdx.x & (kWave - 1));
   const u32x4 lo = ld16(s), hi = ld16(s + 1024);
@@ -506,7 +515,7 @@ __device__ __forceinline__ i32x8 lds_fragment(const uint8_t* tile, int i) {
 }
 
 __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kStages][2][kPageBytes];
+  __shared__ __attribute__((aligned(16))) ManyShared sh;
   int x = blockIdx.x;
   const int split = x % p.splits;
   x /= p.splits;
@@ -522,7 +531,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   Wave w;
   wave_init(p, t, h, t.row0 + kWaveRows * wave, &w);
   const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
+  const uint32_t lds_v = __builtin_amdgcn_readfirstlane(lds_addr(sh.v));
 
   // pages [mid, end) of the part are seen whole by every row of the tile
   int mid, end;
@@ -534,33 +543,49 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
     end = max(min(hi / kPage - t.page_lo, to), mid);
   }
 
-  // Whatever is read of a stage that was never copied to must be finite (where
-  // a page is missing its numerators are made zero).
-  for (int i = threadIdx.x; i < (int)sizeof(lds) / 16; i += kThreads)
-    st16(&lds[0][0][0] + 16 * i, (u32x4){0u, 0u, 0u, 0u});
-  __syncthreads();
+  // V that is read where a page is missing must be finite (its numerators are
+  // made zero, K is zeros): no stage keeps anything but whole pages and zeros.
+  auto clear_v = [&]() __attribute__((always_inline)) {
+    for (int i = threadIdx.x; i < (int)sizeof(sh.v) / 16; i += kThreads)
+      st16(&sh.v[0][0] + 16 * i, (u32x4){0u, 0u, 0u, 0u});
+    __syncthreads();
+  };
+  clear_v();
 
-  // Page n of the part into stage i % 4: 2 KB of K and 2 KB of V per wave, 4
-  // copies a wave (none where there is no page).
-  auto copy = [&](const PageAt& pg, int i) __attribute__((always_inline)) {
+  // V of a page into a stage: 2 KB a wave.
+  auto copy_v = [&](const PageAt& pg, int stage) __attribute__((always_inline)) {
     if (pg.page < 0) return;
-    const int64_t at = ((int64_t)pg.page * p.c.Hkv + h) * kPageBytes;
-    const uint32_t to0 = lds0 + (uint32_t)(i % kStages) * (2 * kPageBytes);
-    const auto kr = make_rsrc(p.c.k8 + at, kPageBytes), vr = make_rsrc(p.c.v8 + at, kPageBytes);
+    const auto r = make_rsrc(p.c.v8 + ((int64_t)pg.page * p.c.Hkv + h) * kPageBytes, kPageBytes);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const uint32_t off = (uint32_t)(2 * wave + j) * 1024u;
-      dma16(to0 + off, kr, off + 16 * lane, 0);
-      dma16(to0 + kPageBytes + off, vr, off + 16 * lane, 0);
+      dma16(lds_v + (uint32_t)stage * kPageBytes + off, r, off + 16 * lane, 0);
     }
   };
-  // This wave's copies are done, but for the 4 newest where `newer`, and none
-  // of its LDS reads is in flight; after the barrier both hold for every wave.
-  auto arrive = [&](bool newer) __attribute__((always_inline)) {
-    if (newer)
-      asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  // This wave's quarter of a page's K (32 keys, 64 channels): its codes, and
+  // those into a stage as bf16.
+  struct Quarter {
+    u32x4 lo, hi;
+  };
+  auto load_k = [&](const PageAt& pg) __attribute__((always_inline)) {
+    const uint8_t* from8 = p.c.k8 + ((int64_t)max(pg.page, 0) * p.c.Hkv + h) * kPageBytes +
+                           2048 * wave + 16 * lane;
+    return Quarter{ld16(from8), ld16(from8 + 1024)};
+  };
+  auto put_k = [&](const Quarter& k, const PageAt& pg, int stage) __attribute__((always_inline)) {
+    const float scale = scale_of(pg.sk);
+    uint8_t* to16 = sh.k[stage] + 4096 * wave + 16 * lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = i < 2 ? k.lo[2 * i] : k.hi[2 * i - 4], b = i < 2 ? k.lo[2 * i + 1] : k.hi[2 * i - 3];
+      const bool there = pg.page >= 0;
+      st16(to16 + 1024 * i, __builtin_bit_cast(u32x4, widen_k(there ? a : 0u, there ? b : 0u, scale)));
+    }
+  };
+  // This wave's copies are done and none of its LDS accesses is in flight; after
+  // the barrier that holds for every wave.
+  auto arrive = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     barrier_keep_loads();
   };
   const PageAt none{-1, kOne, kOne};
@@ -568,32 +593,37 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   auto walk = [&](auto works) __attribute__((always_inline)) {
     // the border pages: from .. mid - 1, then end .. to - 1
     const int borders = (mid - from) + (to - end);
-    PageAt pg0 = none, pg1 = none;
     auto border = [&](int i) __attribute__((always_inline)) {
       return from + i < mid ? from + i : end + i - (mid - from);
     };
+    PageInfo info;
     auto border_info = [&](int i) __attribute__((always_inline)) {
-      const int n = border(i);
-      return page_at(page_info(p.c, table, h, n, 0, to), 0);
+      if ((i & (kWave - 1)) == 0) info = page_info(p.c, table, h, border(i + lane), i + lane < borders);
+      return page_at(info, i & (kWave - 1));
     };
+    PageAt pg0 = none, pg1 = none;
+    Quarter k;
     if (borders > 0) {
       pg0 = border_info(0);
-      copy(pg0, 0);
+      k = load_k(pg0);
+      copy_v(pg0, 0);
     }
     for (int i = 0; i < borders; ++i) {
-      arrive(false);  // page i is there, and the other stage free
+      arrive();  // K and V of page i are there, and the other stages free
+      put_k(k, pg0, i & 1);
       if (i + 1 < borders) {
         pg1 = border_info(i + 1);
-        copy(pg1, (i + 1) & 1);
+        k = load_k(pg1);
+        copy_v(pg1, (i + 1) & 1);
       }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier_keep_loads();
       if constexpr (works.value) {
         if (pg0.page >= 0) {
           const int start = (t.page_lo + border(i)) * kPage;
-          const uint8_t(&tile)[2][kPageBytes] = lds[i & 1];
           f32x16 s[2];
 #pragma unroll
-          for (int rt = 0; rt < 2; ++rt)
-            s[rt] = scores(w, lds_fragment(tile[0], 2 * rt), lds_fragment(tile[0], 2 * rt + 1), pg0.sk);
+          for (int rt = 0; rt < 2; ++rt) s[rt] = lds_scores(w, sh.k[i & 1], rt);
           if (needs_mask(w, start)) mask_scores(w, start, t.sp.keys, s);
           raise_max(w, page_max(s), p.scale_log2);
           const float off = exp_offset(w);
@@ -601,7 +631,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
           numerators(w, p.scale_log2, off, s[0], ph, 0);
           numerators(w, p.scale_log2, off, s[1], ph, 4);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = lds_fragment(tile[1], j);
+          for (int j = 0; j < 4; ++j) f[j] = lds_fragment(sh.v[i & 1], j);
           if (start + kPage > t.sp.keys) clear_tail(f, start, t.sp.keys);
           add_values(w, f, ph, pg0.sv, 0);
           add_values(w, f, rests(s, ph), pg0.sv, kRestP);
@@ -610,54 +640,50 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
       pg0 = pg1;
     }
     if (mid >= end) return;
+    if (borders > 0) {  // the last page may have left codes past the sequence's end
+      arrive();
+      clear_v();
+    }
 
     // the pages seen whole; at step n: pages n .. n + 3
-    PageInfo info = page_info(p.c, table, h, mid, 1, end);
-    auto fetch = [&](int n) __attribute__((always_inline)) {
+    info = page_info(p.c, table, h, mid, 1, end);
+    auto info_of = [&](int n) __attribute__((always_inline)) {  // each n once, in order
+      if (n >= end) return none;
       const int i = (n - mid) & (kWave - 1);
       if (i == 0 && n > mid) info = page_info(p.c, table, h, n, 1, end);
-      const PageAt pg = page_at(info, i);
-      copy(pg, n);
-      return pg;
+      return page_at(info, i);
     };
-    // the last border page may leave codes past the sequence's end in its
-    // stage: the reads of it are over, and a missing page must not meet them
-    arrive(false);
-    if (borders > 0)
-      for (int i = threadIdx.x; i < 4 * kPageBytes / 16; i += kThreads)
-        st16(&lds[0][0][0] + 16 * i, (u32x4){0u, 0u, 0u, 0u});
-    __syncthreads();
-    PageAt pg2 = none;
-    pg0 = fetch(mid);
-    pg1 = mid + 1 < end ? fetch(mid + 1) : none;
-    arrive(mid + 1 < end && pg1.page >= 0);
-    if (mid + 2 < end) pg2 = fetch(mid + 2);
+    pg0 = info_of(mid);
+    pg1 = info_of(mid + 1);
+    PageAt pg2 = info_of(mid + 2);
+    put_k(load_k(pg0), pg0, mid & 1);
+    put_k(load_k(pg1), pg1, (mid + 1) & 1);
+    k = load_k(pg2);
+    copy_v(pg0, mid & 1);
+    arrive();
     f32x16 sa[2], sb[2];  // scores of the current page and of the next
     if constexpr (works.value) {
-      const uint8_t* tile = lds[mid % kStages][0];
-      sa[0] = scores(w, lds_fragment(tile, 0), lds_fragment(tile, 1), pg0.sk);
-      sa[1] = scores(w, lds_fragment(tile, 2), lds_fragment(tile, 3), pg0.sk);
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) sa[rt] = lds_scores(w, sh.k[mid & 1], rt);
       raise_max(w, pg0.page >= 0 ? page_max(sa) : -INFINITY, p.scale_log2);
     }
     auto step = [&](int n, f32x16 (&s)[2], f32x16 (&u)[2]) __attribute__((always_inline)) {
-      arrive(n + 2 < end && pg2.page >= 0);  // page n + 1 is there, and the stage of page n - 1 free
-      PageAt pg3 = none;
-      if (n + 3 < end) pg3 = fetch(n + 3);
+      // V(n) and K(n + 1) can be read, K(n + 2) is in registers, the stages of
+      // K(n) and V(n - 1) are free
+      arrive();
+      put_k(k, pg2, n & 1);
+      const PageAt pg3 = info_of(n + 3);
+      k = load_k(pg3);
+      copy_v(pg1, (n + 1) & 1);
       if constexpr (works.value) {
         const float off = pg0.page >= 0 ? exp_offset(w) : -INFINITY;
-        const uint8_t* kt = lds[(n + 1) % kStages][0];
-        const uint8_t* vt = lds[n % kStages][1];
         i32x8 f[4], ph;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = lds_fragment(kt, i);
-        u[0] = scores(w, f[0], f[1], pg1.sk);
+        u[0] = lds_scores(w, sh.k[(n + 1) & 1], 0);
         numerators(w, p.scale_log2, off, s[0], ph, 0);
-        f[0] = lds_fragment(vt, 0);
-        f[1] = lds_fragment(vt, 1);
-        u[1] = scores(w, f[2], f[3], pg1.sk);
+        u[1] = lds_scores(w, sh.k[(n + 1) & 1], 1);
         numerators(w, p.scale_log2, off, s[1], ph, 4);
-        f[2] = lds_fragment(vt, 2);
-        f[3] = lds_fragment(vt, 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = lds_fragment(sh.v[n & 1], i);
         add_values(w, f, ph, pg0.sv, 0);
         const i32x8 pl = rests(s, ph);
         add_values(w, f, pl, pg0.sv, kRestP);

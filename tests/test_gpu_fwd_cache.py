@@ -1,8 +1,7 @@
 """GPU attention over the paged cache against the float64 reference.
 
-Tolerances, per element.  Scores: 128 products in fp32 (queries split exactly
-but for 2^-23 of their largest element) are off by at most 256 half steps of
-2^-24 of tau |q| |k|, and the exponent's argument by three more half steps of
+Tolerances, per element.  Scores: 128 exact products added in fp32 are off by at
+most 256 half steps of 2^-24 of tau |q| |k|, and the exponent's argument by three more half steps of
 its size, together below ds = 2^-15 tau |q| max|k|.  A probability is off by a
 factor exp(2 ds) and rounded to two e4m3 terms: half an e4m3 step of a rest of
 at most half a step, 2^-4 2^-4 = 2^-8 of it, or half the rest's smallest step,
