@@ -1,14 +1,15 @@
 // Attention of the newest tokens over the paged e4m3 cache, gfx950.
 //
-// Exact softmax attention of bf16 queries over dequantised keys and values.
-// Scores are products of the queries with K widened to bf16, which is exact
-// (four significant bits, a power-of-two scale), with fp32 sums: the fp8 matrix
-// instructions drop low bits of small products, up to 1.3e-5 of a sum's
-// magnitudes, which would be the error of lse.  P . V runs on the fp8 matrix
-// cores, V straight from the cache in operand order, its scale as an E8M0
-// operand; P is split in two e4m3 terms, p = h + l with l the rounded rest: eight
-// significant bits, as in bf16, at the cost of one bf16 product and without
-// converting V.  Row sums take the unrounded probabilities in fp32.
+// Exact softmax attention of bf16 queries over dequantised keys and values, both
+// products on the bf16 matrix cores with fp32 sums.  A code times its page's
+// power-of-two scale is a bf16 number (four significant bits), so K and V are
+// widened exactly, two codes an instruction, in operand order as they lie in the
+// cache.  (Scores on the fp8 matrix cores, the queries split in two e4m3 terms,
+// were 13% faster with many rows, but those instructions drop low bits of small
+// products, up to 1.3e-5 of a sum's magnitudes, which would be the error of lse;
+// probabilities split in two e4m3 terms cost more vector work than widening V.)
+// Probabilities are rounded to bf16 for the product with V, as in the sparse
+// forward; row sums take them unrounded, in fp32.
 //
 // A wave serves 32 rows (a row: one query head of one token; the heads that
 // share a key head are rows side by side).  Two kernels share that step:
@@ -35,14 +36,12 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWaveRows = 32;
 constexpr float kLn2 = 0.69314718055994531f;
-// P is held as 2^6 p in [0, 2^8]: the running maximum may lag by 2^kLazy
-// before the accumulators are rescaled (448 is the largest e4m3 value).
-constexpr float kLogP = 6.f;
-constexpr float kLazy = 2.f;
-// The rests are scaled up: |x - h| is at most half a step, 8 (x <= 256), and
-// 32 (x - h) <= 256.
-constexpr int kRestP = 5;              // log2 of that factor
+// A row's running maximum (log2 units) may lag by this much before what has
+// been summed is rescaled: numerators up to 2^kLazy.
+constexpr float kLazy = 8.f;
 constexpr int kOne = 127;              // E8M0 code of 1
+
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 
 struct Params {
   CacheIn c;
@@ -105,21 +104,6 @@ struct Wave {
   bool valid;
 };
 
-// e4m3 codes of four values.  Each conversion writes half a word; what the
-// word held before does not matter, and no instruction is spent on it.
-__device__ __forceinline__ int cvt4(float a, float b, float c, float d) {
-  int w;
-  asm("" : "=v"(w));
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
-  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-}
-// The rests (x - h) up of four values whose codes h holds, as codes.
-__device__ __forceinline__ int rest4(float x0, float x1, float x2, float x3, int h, float up) {
-  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, up, false);
-  const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, up, true);
-  return cvt4(fmaf(x0, up, -a[0]), fmaf(x1, up, -a[1]), fmaf(x2, up, -b[0]), fmaf(x3, up, -b[1]));
-}
-
 __device__ __forceinline__ float pair_sum32(float x) {
   const uint32_t u = __float_as_uint(x);
   const auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
@@ -149,12 +133,8 @@ __device__ __forceinline__ void wave_init(const Params& p, const Tile& t, int h,
   w->l = 0.f;
 }
 
-#define SA_MFMA(a, b, c, ca, cb) \
-  __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, ca, 0, cb)
-
-// Eight channels of K, of the lane's key, as bf16: codes in two words times the
-// page's scale (exact).
-__device__ __forceinline__ bf16x8 widen_k(uint32_t a, uint32_t b, float scale) {
+// Eight codes in two words, times the page's scale, as bf16 (exact).
+__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float scale) {
   u32x4 o;
   o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false));
   o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true));
@@ -162,8 +142,12 @@ __device__ __forceinline__ bf16x8 widen_k(uint32_t a, uint32_t b, float scale) {
   o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true));
   return __builtin_bit_cast(bf16x8, o);
 }
-// The scale whose E8M0 code is given.
+// The scale whose biased exponent is given.
 __device__ __forceinline__ float scale_of(int code) { return __uint_as_float((uint32_t)code << 23); }
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
 
 // S^T of 32 keys of a page x 32 rows from the fragments of their codes,
 // channels 0-63 and 64-127.
@@ -173,7 +157,7 @@ __device__ __forceinline__ f32x16 scores(const Wave& w, const i32x8& k0, const i
   for (int i = 0; i < 8; ++i) {
     const i32x8& k = i < 4 ? k0 : k1;
     const int j = 2 * (i & 3);
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_k(k[j], k[j + 1], scale), w.q[i], s, 0, 0, 0);
+    s = mfma(widen8(k[j], k[j + 1], scale), w.q[i], s);
   }
   return s;
 }
@@ -217,52 +201,46 @@ __device__ __forceinline__ void raise_max(Wave& w, float mx, float scale_log2) {
       for (int r = 0; r < 16; ++r) w.acc[dt][r] *= a;
   }
 }
-__device__ __forceinline__ float exp_offset(const Wave& w) {
-  return kLogP - (w.m == -INFINITY ? 0.f : w.m);
-}
+// What is subtracted from a row's scores (0 for a row without keys so far).
+__device__ __forceinline__ float exp_ref(const Wave& w) { return w.m == -INFINITY ? 0.f : w.m; }
 
-// Softmax numerators of 32 keys, in place, and their leading e4m3 terms:
-// slots 4 at .. 4 at + 15 of the P operand.
-__device__ __forceinline__ void numerators(Wave& w, float scale_log2, float off, f32x16& s,
-                                           i32x8& ph, int at) {
+// Softmax numerators of 32 keys, added to the row's sum, as bf16: the P operands
+// of keys 0-15 and 16-31 (slot j of the lane's eight: key 16 i + 8 (j / 4) + 4 g +
+// j % 4, V's order in the cache).
+struct Half {
+  bf16x8 p[2];
+};
+__device__ __forceinline__ Half numerators(Wave& w, float scale_log2, float ref, const f32x16& s) {
+  Half h;
 #pragma unroll
-  for (int r = 0; r < 16; r += 4) {
+  for (int i = 0; i < 2; ++i) {
+    u32x4 o;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      s[r + u] = __builtin_amdgcn_exp2f(fmaf(s[r + u], scale_log2, off));
-      w.l += s[r + u];
+    for (int r = 0; r < 4; ++r) {
+      const float a = __builtin_amdgcn_exp2f(fmaf(s[8 * i + 2 * r], scale_log2, -ref));
+      const float b = __builtin_amdgcn_exp2f(fmaf(s[8 * i + 2 * r + 1], scale_log2, -ref));
+      w.l += a;
+      w.l += b;
+      const bf16x2 t = {(__bf16)a, (__bf16)b};
+      o[r] = __builtin_bit_cast(uint32_t, t);
     }
-    ph[at + r / 4] = cvt4(s[r], s[r + 1], s[r + 2], s[r + 3]);
+    h.p[i] = __builtin_bit_cast(bf16x8, o);
   }
-}
-__device__ __forceinline__ i32x8 rests(const f32x16 (&s)[2], const i32x8& ph) {
-  i32x8 pl;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int rt = i >> 2, r = 4 * (i & 3);
-    pl[i] = rest4(s[rt][r], s[rt][r + 1], s[rt][r + 2], s[rt][r + 3], ph[i], (float)(1 << kRestP));
-  }
-  return pl;
+  return h;
 }
 
-// Codes of V at keys at or past `keys` (never written, or left by another
-// sequence: any byte, NaN codes too) become zero.
-__device__ __forceinline__ void clear_tail(i32x8 (&vf)[4], int start, int keys) {
+// Whether a page whose first key is `start` needs the per-score test.
+__device__ __forceinline__ bool needs_mask(const Wave& w, int start) {
+  return start + kPage > w.all_hi || start < w.all_lo;
+}
+
+// Bytes of word j of eight of V's codes that belong to keys below `keys` (page's
+// first key: start).  Those at or past it (never written, or left by another
+// sequence: any byte, NaN codes too) are taken as zero.
+__device__ __forceinline__ uint32_t tail_mask(int j, int start, int keys) {
   const int g = (threadIdx.x >> 5) & 1;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int left = keys - start - (32 * (j >> 2) + 8 * (j & 3) + 4 * g);
-    const uint32_t m = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) vf[dt][j] &= (int)m;
-  }
-}
-
-// O^T += V^T . P^T of one term of P; rest: log2 of its factor.
-__device__ __forceinline__ void add_values(Wave& w, const i32x8 (&vf)[4], const i32x8& p, int sv,
-                                           int rest) {
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt) w.acc[dt] = SA_MFMA(vf[dt], p, w.acc[dt], sv, kOne - rest);
+  const int left = keys - start - (32 * (j >> 2) + 8 * (j & 3) + 4 * g);
+  return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 }
 
 // 64 pages of a range, one a lane: the pool's page (-1: none) and the E8M0
@@ -298,11 +276,6 @@ __device__ __forceinline__ PageAt page_at(const PageInfo& f, int lane) {
   return {__builtin_amdgcn_readlane(f.page, lane), s & 0xff, s >> 8};
 }
 
-// Whether a page whose first key is `start` needs the per-score test.
-__device__ __forceinline__ bool needs_mask(const Wave& w, int start) {
-  return start + kPage > w.all_hi || start < w.all_lo;
-}
-
 // Row of four consecutive channels: bf16 of x * inv.
 __device__ __forceinline__ void store4(uint16_t* o, const float (&x)[4], float inv) {
   u32x2 v;
@@ -312,7 +285,7 @@ __device__ __forceinline__ void store4(uint16_t* o, const float (&x)[4], float i
 }
 
 __device__ __forceinline__ float lse_of(float m, float l) {
-  return l > 0.f ? (m + __builtin_amdgcn_logf(l) - kLogP) * kLn2 : -INFINITY;
+  return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // Channels 32 dt .. +31 of the wave's rows, their sums l over all keys of the
@@ -395,8 +368,8 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
     for (int i = 0; i < mine; ++i) {
       const int n = from + wave + kWaves * i, start = (t.page_lo + n) * kPage;
       const int scales = __builtin_amdgcn_readlane(info.scales, i & (kWave - 1));
-      const float sk = scale_of(scales & 0xff);
-      const int sv = scales >> 8, j = (i + 1) & (kWave - 1);
+      const float sk = scale_of(scales & 0xff), sv = scale_of(scales >> 8);
+      const int j = (i + 1) & (kWave - 1);
       if (j == 0 && i + 1 < mine) info = page_info(p.c, table, h, n + kWaves, kWaves, to);
       // after the last page every lane asks for the same few bytes again, which
       // costs less than a branch here
@@ -411,14 +384,23 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
       const int keys = page >= 0 ? t.sp.keys : start;  // none of a missing page
       if (start + kPage > keys || needs_mask(w, start)) mask_scores(w, start, keys, s);
       raise_max(w, page_max(s), p.scale_log2);
-      const float off = exp_offset(w);
-      i32x8 ph;
-      numerators(w, p.scale_log2, off, s[0], ph, 0);
-      numerators(w, p.scale_log2, off, s[1], ph, 4);
-      const i32x8 pl = rests(s, ph);
-      if (start + kPage > keys) clear_tail(vf, start, keys);
-      add_values(w, vf, ph, sv, 0);
-      add_values(w, vf, pl, sv, kRestP);
+      const float ref = exp_ref(w);
+      const Half p0 = numerators(w, p.scale_log2, ref, s[0]);
+      const Half p1 = numerators(w, p.scale_log2, ref, s[1]);
+      if (start + kPage > keys) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const uint32_t m = tail_mask(x, start, keys);
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) vf[dt][x] &= (int)m;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+          w.acc[dt] = mfma(widen8(vf[dt][2 * x], vf[dt][2 * x + 1], sv),
+                           (x < 2 ? p0 : p1).p[x & 1], w.acc[dt]);
       load_fragments(vf, p.c.v8 + at, lane16);
       page = next;
     }
@@ -476,42 +458,39 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
 }
 
 // ---- many rows ----------------------------------------------------------------
-// The four waves share every page through LDS: K widened to bf16 by a quarter
-// each, V as it is.  Most pages are seen whole by every row of the tile: they
-// form one range, and go through a loop without masks or branches whose steps
-// hold matrix work and independent vector work side by side: S(n + 1) beside the
-// numerators of page n, the products of P(n)'s leading terms beside their rests,
-// those of the rests beside the maxima of S(n + 1).  (Spelling the order of the
-// two out, with scheduling groups of 14 vector instructions a product, made it
-// 3% slower.)  The pages before and after that range (causal borders, the
-// sequence's last page) come first, one by one.
+// The four waves share every page through LDS, widened to bf16 by a quarter
+// each.  Most pages are seen whole by every row of the tile: they form one
+// range, and go through a loop without masks or branches whose steps hold matrix
+// work and independent vector work side by side: S(n + 1) beside the numerators
+// of page n, the products of P(n) beside the maxima of S(n + 1).  (Spelling the
+// order of the two out, with scheduling groups of 14 vector instructions a
+// product, made it 3% slower.)  The pages before and after that range (causal
+// borders, the sequence's last page) come first, one by one; so do all of them
+// where the table misses one.
 constexpr int kManyRows = kWaves * kWaveRows;
 
+// A page's K or V as bf16: 16 pieces of 64 x 16 bytes in operand order, K by 32
+// keys and 16 channels, V by 32 channels and 16 keys.
+constexpr int kWideBytes = 2 * kPageBytes;
 struct ManyShared {
-  uint8_t k[2][2 * kPageBytes];  // bf16: 1 KB for each (32 keys, 16 channels) in operand order
-  uint8_t v[2][kPageBytes];
+  uint8_t k[2][kWideBytes], v[2][kWideBytes];
 };
-
+__device__ __forceinline__ bf16x8 piece(const uint8_t* wide, int i) {
+  return __builtin_bit_cast(bf16x8, ld16(wide + 1024 * i + 16 * (threadIdx.x & (kWave - 1))));
+}
 // S^T of 32 keys (rt: which) of a page in LDS.
 __device__ __forceinline__ f32x16 lds_scores(const Wave& w, const uint8_t* k, int rt) {
   f32x16 s = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-        __builtin_bit_cast(bf16x8, ld16(k + 1024 * (8 * rt + i) + 16 * (threadIdx.x & (kWave - 1)))),
-        w.q[i], s, 0, 0, 0);
+  for (int i = 0; i < 8; ++i) s = mfma(piece(k, 8 * rt + i), w.q[i], s);
   return s;
 }
-__device__ __forceinline__ i32x8 lds_fragment(const uint8_t* tile, int i) {
-  const uint8_t* s = tile + 2048 * i + 16 * (threadIdx.x & (kWave - 1));
-  const u32x4 lo = ld16(s), hi = ld16(s + 1024);
-  i32x8 f;
+// O^T += V^T . P^T of 32 keys (rt) of a page in LDS.
+__device__ __forceinline__ void lds_values(Wave& w, const uint8_t* v, int rt, const Half& h) {
 #pragma unroll
-  for (int y = 0; y < 4; ++y) {
-    f[y] = (int)lo[y];
-    f[4 + y] = (int)hi[y];
-  }
-  return f;
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) w.acc[dt] = mfma(piece(v, 4 * dt + 2 * rt + i), h.p[i], w.acc[dt]);
 }
 
 __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
@@ -531,9 +510,8 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   Wave w;
   wave_init(p, t, h, t.row0 + kWaveRows * wave, &w);
   const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
-  const uint32_t lds_v = __builtin_amdgcn_readfirstlane(lds_addr(sh.v));
 
-  // pages [mid, end) of the part are seen whole by every row of the tile
+  // pages [mid, end) of the part are there and seen whole by every row of the tile
   int mid, end;
   {
     int lo, hi, lo1, hi1;
@@ -541,51 +519,39 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
     visible(p.c, t.sp.pos0 + (min(t.row0 + kManyRows, t.rows) - 1) / p.c.g, t.sp.keys, &lo1, &hi1);
     mid = min(max((int)(((int64_t)lo1 + kPage - 1) / kPage) - t.page_lo, from), to);
     end = max(min(hi / kPage - t.page_lo, to), mid);
+    bool missing = false;
+    for (int n = mid + lane; n < end; n += kWave) {
+      const int page = table[n];
+      missing |= page < 0 || page >= p.c.P;
+    }
+    if (__any(missing)) mid = end = to;
   }
 
-  // V that is read where a page is missing must be finite (its numerators are
-  // made zero, K is zeros): no stage keeps anything but whole pages and zeros.
-  auto clear_v = [&]() __attribute__((always_inline)) {
-    for (int i = threadIdx.x; i < (int)sizeof(sh.v) / 16; i += kThreads)
-      st16(&sh.v[0][0] + 16 * i, (u32x4){0u, 0u, 0u, 0u});
-    __syncthreads();
-  };
-  clear_v();
-
-  // V of a page into a stage: 2 KB a wave.
-  auto copy_v = [&](const PageAt& pg, int stage) __attribute__((always_inline)) {
-    if (pg.page < 0) return;
-    const auto r = make_rsrc(p.c.v8 + ((int64_t)pg.page * p.c.Hkv + h) * kPageBytes, kPageBytes);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t off = (uint32_t)(2 * wave + j) * 1024u;
-      dma16(lds_v + (uint32_t)stage * kPageBytes + off, r, off + 16 * lane, 0);
-    }
-  };
-  // This wave's quarter of a page's K (32 keys, 64 channels): its codes, and
+  // This wave's quarter of a page's K (32 keys, 64 channels) or V (32 channels):
+  // its codes (page 0's where there is none, of which nothing is used), and
   // those into a stage as bf16.
   struct Quarter {
     u32x4 lo, hi;
   };
-  auto load_k = [&](const PageAt& pg) __attribute__((always_inline)) {
-    const uint8_t* from8 = p.c.k8 + ((int64_t)max(pg.page, 0) * p.c.Hkv + h) * kPageBytes +
-                           2048 * wave + 16 * lane;
-    return Quarter{ld16(from8), ld16(from8 + 1024)};
+  auto load = [&](const uint8_t* pool, const PageAt& pg) __attribute__((always_inline)) {
+    const uint8_t* at = pool + ((int64_t)max(pg.page, 0) * p.c.Hkv + h) * kPageBytes + 2048 * wave +
+                        16 * lane;
+    return Quarter{ld16(at), ld16(at + 1024)};
   };
-  auto put_k = [&](const Quarter& k, const PageAt& pg, int stage) __attribute__((always_inline)) {
-    const float scale = scale_of(pg.sk);
-    uint8_t* to16 = sh.k[stage] + 4096 * wave + 16 * lane;
+  auto put = [&](uint8_t* wide, const Quarter& q, int code) __attribute__((always_inline)) {
+    const float scale = scale_of(code);
+    uint8_t* to16 = wide + 4096 * wave + 16 * lane;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t a = i < 2 ? k.lo[2 * i] : k.hi[2 * i - 4], b = i < 2 ? k.lo[2 * i + 1] : k.hi[2 * i - 3];
-      const bool there = pg.page >= 0;
-      st16(to16 + 1024 * i, __builtin_bit_cast(u32x4, widen_k(there ? a : 0u, there ? b : 0u, scale)));
+      const u32x4& c = i < 2 ? q.lo : q.hi;
+      st16(to16 + 1024 * i,
+           __builtin_bit_cast(u32x4, widen8(c[2 * (i & 1)], c[2 * (i & 1) + 1], scale)));
     }
   };
-  // This wave's copies are done and none of its LDS accesses is in flight; after
-  // the barrier that holds for every wave.
-  auto arrive = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  // None of this wave's LDS accesses is in flight; after the barrier that holds
+  // for every wave (loads of pages to come stay in flight).
+  auto meet = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     barrier_keep_loads();
   };
   const PageAt none{-1, kOne, kOne};
@@ -602,48 +568,45 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
       return page_at(info, i & (kWave - 1));
     };
     PageAt pg0 = none, pg1 = none;
-    Quarter k;
+    Quarter k, v;
     if (borders > 0) {
       pg0 = border_info(0);
-      k = load_k(pg0);
-      copy_v(pg0, 0);
+      k = load(p.c.k8, pg0);
+      v = load(p.c.v8, pg0);
     }
     for (int i = 0; i < borders; ++i) {
-      arrive();  // K and V of page i are there, and the other stages free
-      put_k(k, pg0, i & 1);
+      const int start = (t.page_lo + border(i)) * kPage;
+      if (start + kPage > t.sp.keys) {  // (words 0-3 of V: keys 0-31)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          v.lo[y] &= tail_mask(y, start, t.sp.keys);
+          v.hi[y] &= tail_mask(4 + y, start, t.sp.keys);
+        }
+      }
+      put(sh.k[i & 1], k, pg0.sk);
+      put(sh.v[i & 1], v, pg0.sv);
       if (i + 1 < borders) {
         pg1 = border_info(i + 1);
-        k = load_k(pg1);
-        copy_v(pg1, (i + 1) & 1);
+        k = load(p.c.k8, pg1);
+        v = load(p.c.v8, pg1);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      barrier_keep_loads();
+      meet();  // page i is there; the other stages have been read
       if constexpr (works.value) {
         if (pg0.page >= 0) {
-          const int start = (t.page_lo + border(i)) * kPage;
           f32x16 s[2];
 #pragma unroll
           for (int rt = 0; rt < 2; ++rt) s[rt] = lds_scores(w, sh.k[i & 1], rt);
           if (needs_mask(w, start)) mask_scores(w, start, t.sp.keys, s);
           raise_max(w, page_max(s), p.scale_log2);
-          const float off = exp_offset(w);
-          i32x8 ph, f[4];
-          numerators(w, p.scale_log2, off, s[0], ph, 0);
-          numerators(w, p.scale_log2, off, s[1], ph, 4);
+          const float ref = exp_ref(w);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = lds_fragment(sh.v[i & 1], j);
-          if (start + kPage > t.sp.keys) clear_tail(f, start, t.sp.keys);
-          add_values(w, f, ph, pg0.sv, 0);
-          add_values(w, f, rests(s, ph), pg0.sv, kRestP);
+          for (int rt = 0; rt < 2; ++rt)
+            lds_values(w, sh.v[i & 1], rt, numerators(w, p.scale_log2, ref, s[rt]));
         }
       }
       pg0 = pg1;
     }
     if (mid >= end) return;
-    if (borders > 0) {  // the last page may have left codes past the sequence's end
-      arrive();
-      clear_v();
-    }
 
     // the pages seen whole; at step n: pages n .. n + 3
     info = page_info(p.c, table, h, mid, 1, end);
@@ -656,41 +619,38 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
     pg0 = info_of(mid);
     pg1 = info_of(mid + 1);
     PageAt pg2 = info_of(mid + 2);
-    put_k(load_k(pg0), pg0, mid & 1);
-    put_k(load_k(pg1), pg1, (mid + 1) & 1);
-    k = load_k(pg2);
-    copy_v(pg0, mid & 1);
-    arrive();
+    meet();
+    put(sh.k[mid & 1], load(p.c.k8, pg0), pg0.sk);
+    put(sh.k[(mid + 1) & 1], load(p.c.k8, pg1), pg1.sk);
+    put(sh.v[mid & 1], load(p.c.v8, pg0), pg0.sv);
+    k = load(p.c.k8, pg2);
+    v = load(p.c.v8, pg1);
+    meet();
     f32x16 sa[2], sb[2];  // scores of the current page and of the next
     if constexpr (works.value) {
 #pragma unroll
       for (int rt = 0; rt < 2; ++rt) sa[rt] = lds_scores(w, sh.k[mid & 1], rt);
-      raise_max(w, pg0.page >= 0 ? page_max(sa) : -INFINITY, p.scale_log2);
+      raise_max(w, page_max(sa), p.scale_log2);
     }
     auto step = [&](int n, f32x16 (&s)[2], f32x16 (&u)[2]) __attribute__((always_inline)) {
-      // V(n) and K(n + 1) can be read, K(n + 2) is in registers, the stages of
-      // K(n) and V(n - 1) are free
-      arrive();
-      put_k(k, pg2, n & 1);
+      meet();  // V(n) and K(n + 1) are there, the stages of K(n) and V(n - 1) free
+      put(sh.k[n & 1], k, pg2.sk);
+      put(sh.v[(n + 1) & 1], v, pg1.sv);
       const PageAt pg3 = info_of(n + 3);
-      k = load_k(pg3);
-      copy_v(pg1, (n + 1) & 1);
+      k = load(p.c.k8, pg3);
+      v = load(p.c.v8, pg2);
       if constexpr (works.value) {
-        const float off = pg0.page >= 0 ? exp_offset(w) : -INFINITY;
-        i32x8 f[4], ph;
+        const float ref = w.m;
         u[0] = lds_scores(w, sh.k[(n + 1) & 1], 0);
-        numerators(w, p.scale_log2, off, s[0], ph, 0);
+        const Half p0 = numerators(w, p.scale_log2, ref, s[0]);
         u[1] = lds_scores(w, sh.k[(n + 1) & 1], 1);
-        numerators(w, p.scale_log2, off, s[1], ph, 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = lds_fragment(sh.v[n & 1], i);
-        add_values(w, f, ph, pg0.sv, 0);
-        const i32x8 pl = rests(s, ph);
-        add_values(w, f, pl, pg0.sv, kRestP);
+        const Half p1 = numerators(w, p.scale_log2, ref, s[1]);
+        lds_values(w, sh.v[n & 1], 0, p0);
+        lds_values(w, sh.v[n & 1], 1, p1);
         float mx = page_max(u);
         // (taken unconditionally: a branch here would pull the step apart)
         asm volatile("" : "+v"(mx));
-        raise_max(w, n + 1 < end && pg1.page >= 0 ? mx : -INFINITY, p.scale_log2);
+        raise_max(w, n + 1 < end ? mx : -INFINITY, p.scale_log2);
       }
       pg0 = pg1;
       pg1 = pg2;
@@ -703,7 +663,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   };
   if (t.row0 + kWaveRows * wave < t.rows) {
     walk(std::true_type{});
-  } else {  // no rows: this wave copies its share and keeps the barriers
+  } else {  // no rows: this wave widens its share and keeps the barriers
     walk(std::false_type{});
     return;
   }
