@@ -18,11 +18,10 @@
 //              registers, the next page's while one is worked on, and merge
 //              their softmax states through LDS.  One token over 524,288 (40
 //              heads on 8): 170 us, 6.3 TB/s of the cache's bytes
-//   many rows  bound by the matrix cores and the vector work beside them; four
-//              waves of 32 rows share every page through LDS, copied up to
-//              three pages ahead.  4,680 tokens over 32,760 (12 heads): 0.94 ms,
-//              1,000 TFLOP/s (a large bf16 library product: 1,380), matrix
-//              cores busy 43% of the cycles, vector units 57%, at 2.05 GHz
+//   many rows  bound by LDS reads, the matrix cores and the vector work beside
+//              them; four waves of 32 rows share every page through LDS.  4,680
+//              tokens over 32,760 (12 heads): 0.92 ms, 1,020 TFLOP/s (a large
+//              bf16 library product: 1,380)
 // Long key ranges are cut over workgroups when there are few rows: partial
 // sums go to the workspace and a second kernel joins them in a fixed order.
 #include <type_traits>
@@ -320,17 +319,17 @@ __device__ __forceinline__ void store_sums(const Params& p, const Wave& w, float
 // ---- few rows ---------------------------------------------------------------
 constexpr int kFewRows = 32;
 
-__device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* tile, int at) {
+__device__ __forceinline__ void load_fragment(i32x8& f, const uint8_t* at) {
+  const u32x4 lo = ld16_once(at), hi = ld16_once(at + 1024);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const u32x4 lo = ld16_once(tile + 2048 * i + at);
-    const u32x4 hi = ld16_once(tile + 2048 * i + 1024 + at);
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      f[i][x] = (int)lo[x];
-      f[i][4 + x] = (int)hi[x];
-    }
+  for (int x = 0; x < 4; ++x) {
+    f[x] = (int)lo[x];
+    f[4 + x] = (int)hi[x];
   }
+}
+__device__ __forceinline__ void load_fragments(i32x8 (&f)[4], const uint8_t* at) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) load_fragment(f[i], at + 2048 * i);
 }
 
 __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
@@ -350,9 +349,10 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
   Wave w;
   const int32_t* table = p.c.pages + (int64_t)t.b * p.c.pages_stride + t.page_lo;
 
-  // pages from + wave + 4 i, 64 of them known at a time; K of the next one loads
-  // once S has been computed, V once it has been multiplied, into the same
-  // registers (where there is no page, page 0's tiles, of which nothing is used)
+  // pages from + wave + 4 i, 64 of them known at a time; each fragment of the next
+  // one loads into the registers of this one's as soon as that has been multiplied
+  // (K's and V's each in one go, once all of it has been: 4% slower; where there is
+  // no page, page 0's tiles, of which nothing is used)
   const int mine = to > from + wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
   auto tile_at = [&](int page) __attribute__((always_inline)) {
     return ((int64_t)max(page, 0) * p.c.Hkv + h) * kPageBytes;
@@ -362,8 +362,8 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
     int page = __builtin_amdgcn_readlane(info.page, 0);
     i32x8 kf[4], vf[4];
     const int mine16 = 16 * (threadIdx.x & (kWave - 1));  // this lane's bytes of a fragment
-    load_fragments(kf, p.c.k8 + tile_at(page), mine16);
-    load_fragments(vf, p.c.v8 + tile_at(page), mine16);
+    load_fragments(kf, p.c.k8 + tile_at(page) + mine16);
+    load_fragments(vf, p.c.v8 + tile_at(page) + mine16);
     wave_init(p, t, h, t.row0, &w);
     for (int i = 0; i < mine; ++i) {
       const int n = from + wave + kWaves * i, start = (t.page_lo + n) * kPage;
@@ -375,12 +375,11 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
       // costs less than a branch here
       const bool more = i + 1 < mine;
       const int next = more ? __builtin_amdgcn_readlane(info.page, j) : page;
-      const int64_t at = tile_at(next);
-      const int lane16 = more ? mine16 : 0;
+      const int64_t at = tile_at(next) + (more ? mine16 : 0);
       f32x16 s[2];
       s[0] = scores(w, kf[0], kf[1], sk);
       s[1] = scores(w, kf[2], kf[3], sk);
-      load_fragments(kf, p.c.k8 + at, lane16);
+      load_fragments(kf, p.c.k8 + at);
       const int keys = page >= 0 ? t.sp.keys : start;  // none of a missing page
       if (start + kPage > keys || needs_mask(w, start)) mask_scores(w, start, keys, s);
       raise_max(w, page_max(s), p.scale_log2);
@@ -396,12 +395,13 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_few_kernel(Params p) {
         }
       }
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+      for (int dt = 0; dt < 4; ++dt) {
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
+        for (int x = 0; x < 4; ++x)
           w.acc[dt] = mfma(widen8(vf[dt][2 * x], vf[dt][2 * x + 1], sv),
                            (x < 2 ? p0 : p1).p[x & 1], w.acc[dt]);
-      load_fragments(vf, p.c.v8 + at, lane16);
+        load_fragment(vf[dt], p.c.v8 + at + 2048 * dt);
+      }
       page = next;
     }
   } else {
@@ -641,6 +641,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
       v = load(p.c.v8, pg2);
       if constexpr (works.value) {
         const float ref = w.m;
+        __builtin_amdgcn_s_setprio(1);  // until the next barrier: 2% faster
         u[0] = lds_scores(w, sh.k[(n + 1) & 1], 0);
         const Half p0 = numerators(w, p.scale_log2, ref, s[0]);
         u[1] = lds_scores(w, sh.k[(n + 1) & 1], 1);
@@ -651,6 +652,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
         // (taken unconditionally: a branch here would pull the step apart)
         asm volatile("" : "+v"(mx));
         raise_max(w, n + 1 < end ? mx : -INFINITY, p.scale_log2);
+        __builtin_amdgcn_s_setprio(0);
       }
       pg0 = pg1;
       pg1 = pg2;
