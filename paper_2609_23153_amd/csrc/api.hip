@@ -4,6 +4,8 @@
 #include <math.h>
 
 #include "launch.h"
+#include "launch_cache.h"
+#include "launch_norm.h"
 #include "sparse_attn.h"
 
 namespace {

@@ -2,8 +2,8 @@
 // sequence a workgroup serves, where its tokens stand, which keys they see.
 #pragma once
 
-#include "common.h"
-#include "launch.h"
+#include "launch_cache.h"
+#include "rows.h"
 
 namespace sa {
 

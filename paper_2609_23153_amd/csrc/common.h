@@ -64,11 +64,6 @@ __device__ __forceinline__ void barrier_keep_loads() { asm volatile("s_barrier" 
 __device__ __forceinline__ u32x4 ld16(const void* p) {
   return *reinterpret_cast<const u32x4*>(p);
 }
-// The same for data that is read once: it does not push out what the caches
-// hold (one token over a long cache: 5.5 -> 6.2 TB/s).
-__device__ __forceinline__ u32x4 ld16_once(const void* p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-}
 __device__ __forceinline__ void st16(void* p, u32x4 v) { *reinterpret_cast<u32x4*>(p) = v; }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -108,24 +103,6 @@ __device__ __forceinline__ uint32_t wave_sum_u32(uint32_t x) {
   x = p[0] + p[1];
   const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
   return q[0] + q[1];
-}
-
-// The same for floats.
-__device__ __forceinline__ float wave_sum_f32(float x) {
-#define SA_ROR(n)                                                                              \
-  x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + n, \
-                                                             0xF, 0xF, false))
-  SA_ROR(8);
-  SA_ROR(4);
-  SA_ROR(2);
-  SA_ROR(1);
-#undef SA_ROR
-  const uint32_t u = __float_as_uint(x);
-  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-  const uint32_t v = __float_as_uint(x);
-  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
 // Whole-wave reductions through DPP-free cross-lane shuffles.

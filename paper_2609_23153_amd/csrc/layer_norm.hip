@@ -13,8 +13,8 @@
 // in a fixed order: no atomics, the same bits every time.
 #include <type_traits>
 
-#include "common.h"
-#include "launch.h"
+#include "launch_norm.h"
+#include "rows.h"
 
 namespace sa {
 namespace {
