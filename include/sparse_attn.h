@@ -400,18 +400,20 @@ int sparse_attn_linear_w8a8(const uint8_t* xq, const float* sx, int64_t ldx, con
  *              head j / (heads / kv_heads)
  *  head_dim    must be 128
  *  tokens      T >= 0 rows of the packed tensors: row q_start[b] + i is the
- *              i-th new token of sequence b
+ *              i-th new token of sequence b.  T heads <= 2^28, B heads <= 2^22
  *  num_pages   pages P >= 1 of the pool
  *  max_pages   entries of a page-table row, 1 <= max_pages < 2^24
  *  pages_stride  elements from one page-table row to the next (>= max_pages)
- *  *_stride    element strides of (token, head), channels contiguous
+ *  *_stride    element strides of (token, head), channels contiguous; rows that
+ *              are written must not overlap
  *  softmax_scale, causal_chunk, causal_window  as in sparse_attn_desc (the
  *              position of a token in its sequence decides its chunk)
  * Device tensors of a cache, contiguous but for the table's rows:
  *  k8, v8      uint8 [P][kv_heads][8192];  sk, sv  fp32 [P][kv_heads]
  *  pages       int32 [B][max_pages]: tokens 64 j .. 64 j + 63 of sequence b are
  *              in page pages[b][j].  Entries outside [0, P) name no page:
- *              their tokens are not stored and not attended
+ *              their tokens, and those past the table's end, are not stored
+ *              and not attended
  *  q_start     int32 [B + 1], non-decreasing, within [0, T] (kept there)
  *  kv_len      int32 [B]: tokens of the sequence, its n = q_start[b + 1] -
  *              q_start[b] new ones (the last n positions) among them
@@ -433,7 +435,8 @@ typedef struct {
 
 /*
  * Appends the packed new tokens' keys and values to the cache.
- *  k, v     bf16 [T][kv_heads][128] via k_stride, v_stride
+ *  k, v     bf16 [T][kv_heads][128] via k_stride, v_stride, finite (an infinite
+ *           one takes the page's other codes of its head with it)
  *  rope     fp32 [rope_rows][rope_dim / 2][2] (cos, sin), or NULL: every key is
  *           rotated in its first rope_dim channels (a multiple of 8, at most
  *           128), pairs (2m, 2m+1) as (a c - b s, a s + b c), each fp32
@@ -474,9 +477,10 @@ size_t sparse_attn_fwd_cache_workspace_size(const sparse_attn_cache_desc* desc);
  * on the dequantised keys and values; a query that sees no key gets o = 0 and
  * lse = -inf.  Products accumulate in fp32; queries, keys and values enter
  * exactly, the probabilities rounded to 8 significant bits, the row sums
- * unrounded.  Cached tokens that some query of
- * the call sees must be finite; the slots behind the last token may hold
- * anything.  Call sparse_attn_cache_append for the new tokens first.
+ * unrounded.  A sequence's cached
+ * tokens must be finite in every page that some query of the call sees a key
+ * of; the slots behind the last token may hold anything.  Several sequences may
+ * share pages.  Call sparse_attn_cache_append for the new tokens first.
  *  q, o     bf16 [T][heads][128] via q_stride, o_stride; o must not overlap q
  *  lse      fp32 [T][heads] out, contiguous; may be NULL
  *  ws       ws_bytes >= sparse_attn_fwd_cache_workspace_size()

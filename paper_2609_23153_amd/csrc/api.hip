@@ -426,6 +426,11 @@ bool strides2_ok(const int64_t st[2]) {
   return st[0] >= 0 && (st[0] & 7) == 0 && st[1] >= 0 && (st[1] & 7) == 0;
 }
 
+// Rows of 128 channels that are written must not lie on each other.
+bool out_strides_ok(const int64_t st[2], int64_t tokens, int64_t heads) {
+  return strides2_ok(st) && (tokens <= 1 || st[0] >= 128) && (heads <= 1 || st[1] >= 128);
+}
+
 int check_cache_desc(const sparse_attn_cache_desc* d, sa::CacheIn* c) {
   if (!d) return SA_ERR_INVALID_ARG;
   if (d->batch < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
@@ -435,8 +440,9 @@ int check_cache_desc(const sparse_attn_cache_desc* d, sa::CacheIn* c) {
   if (d->causal_chunk < 0 || d->causal_window < 0) return SA_ERR_INVALID_ARG;
   if (d->causal_chunk == 0 && d->causal_window != 0) return SA_ERR_INVALID_ARG;
   if (d->head_dim != 128) return SA_ERR_UNSUPPORTED;
-  // packed rows and work items are counted in 32 bits, token positions too
-  const int64_t most = (int64_t)1 << 30;
+  // a launch holds fewer than 2^32 threads, 256 per work item: T heads / 64 + 2 B heads
+  // of the append, T heads / 32 + B heads and at most twice B heads of the attention
+  const int64_t most = (int64_t)1 << 28;
   if ((int64_t)d->tokens * d->heads > most || (int64_t)d->batch * d->heads > most / 64 ||
       d->max_pages >= (1 << 24))
     return SA_ERR_UNSUPPORTED;
@@ -485,7 +491,9 @@ int sparse_attn_cache_append(const sparse_attn_cache_desc* desc, const void* k, 
   if (in.c.T > 0 && !q != !q_out) return SA_ERR_INVALID_ARG;
   if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out)) return SA_ERR_INVALID_ARG;
   if (!strides2_ok(desc->k_stride) || !strides2_ok(desc->v_stride)) return SA_ERR_INVALID_ARG;
-  if (q && (!strides2_ok(desc->q_stride) || !strides2_ok(desc->o_stride))) return SA_ERR_INVALID_ARG;
+  if (q && (!strides2_ok(desc->q_stride) ||
+            !out_strides_ok(desc->o_stride, desc->tokens, desc->heads)))
+    return SA_ERR_INVALID_ARG;
   if (q && q == q_out &&
       (desc->q_stride[0] != desc->o_stride[0] || desc->q_stride[1] != desc->o_stride[1]))
     return SA_ERR_INVALID_ARG;
@@ -531,7 +539,9 @@ int sparse_attn_fwd_cache(const sparse_attn_cache_desc* desc, const void* q, con
   if (!ws || !aligned16(ws) || !aligned16(q) || !aligned16(o) ||
       (reinterpret_cast<uintptr_t>(lse) & 3u) != 0)
     return SA_ERR_INVALID_ARG;
-  if (!strides2_ok(desc->q_stride) || !strides2_ok(desc->o_stride)) return SA_ERR_INVALID_ARG;
+  if (!strides2_ok(desc->q_stride) ||
+      !out_strides_ok(desc->o_stride, desc->tokens, desc->heads))
+    return SA_ERR_INVALID_ARG;
   if (ws_bytes < sa::fwd_cache_workspace_bytes(in.c)) return SA_ERR_WORKSPACE;
   in.q = static_cast<const uint16_t*>(q);
   in.o = static_cast<uint16_t*>(o);

@@ -109,6 +109,8 @@ BAD_CACHE_DESCS = [
     (dict(softmax_scale=-1.0), INVALID), (dict(softmax_scale=float("nan")), INVALID),
     (dict(max_pages=1 << 24, pages_stride=1 << 24), UNSUPPORTED),
     (dict(tokens=(1 << 27) + 1), UNSUPPORTED), (dict(batch=1 << 22), UNSUPPORTED),
+    (dict(tokens=(1 << 25) + 1), UNSUPPORTED), (dict(batch=(1 << 19) + 1), UNSUPPORTED),
+    (dict(o_stride=(0, 128)), INVALID), (dict(o_stride=(1024, 120)), INVALID),   # rows overlap
 ]
 
 
@@ -202,6 +204,8 @@ def test_fwd_cache_workspace():
     assert size(heads=6) == 0 and size(head_dim=64) == 0
     assert sa.library().sparse_attn_fwd_cache_workspace_size(None) == 0
     assert size() >= 16 and size(tokens=0) >= 16
+    assert size(tokens=1 << 25) > 0 and size(tokens=(1 << 25) + 1) == 0
+    assert size(batch=1 << 19) > 0 and size(batch=(1 << 19) + 1) == 0
     # parts are bounded: one long sequence, 64 of them
     one = size(batch=1, tokens=1, max_pages=1 << 20, pages_stride=1 << 20)
     assert one == 64 * 8 * (128 * 4 + 8)
