@@ -732,9 +732,9 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
 // the cache's bytes.  A part is given at least one page a wave where there are
 // not enough workgroups for every CU, four where there are (its start and end
 // cost about as much as two pages).
-// Short tables are not cut: one token over 24 pages of 12 heads takes 12.7 us in
-// a stream of calls and 32 alone whole, 15.6 and 30 in parts; over 32 pages 15.1
-// and 34, in parts 15.8 and 30.
+// Short tables are not cut: one token over 24 pages of 12 heads takes 13.0 us in
+// a stream of calls, 30 alone and 10.6 in a captured graph whole, 15.7, 29 and
+// 9.5 in parts; over 48 pages 16.5, 36 and 17, in parts 15.7, 30 and 9.8.
 constexpr int kWhole = 24;  // pages
 struct Plan {
   bool few;
