@@ -435,8 +435,9 @@ typedef struct {
 
 /*
  * Appends the packed new tokens' keys and values to the cache.
- *  k, v     bf16 [T][kv_heads][128] via k_stride, v_stride, finite (an infinite
- *           one takes the page's other codes of its head with it)
+ *  k, v     bf16 [T][kv_heads][128] via k_stride, v_stride, below 2^127 in
+ *           magnitude (an infinite one takes the page's other codes of its head
+ *           with it)
  *  rope     fp32 [rope_rows][rope_dim / 2][2] (cos, sin), or NULL: every key is
  *           rotated in its first rope_dim channels (a multiple of 8, at most
  *           128), pairs (2m, 2m+1) as (a c - b s, a s + b c), each fp32

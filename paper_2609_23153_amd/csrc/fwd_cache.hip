@@ -2,14 +2,14 @@
 //
 // Exact softmax attention of bf16 queries over dequantised keys and values, both
 // products on the bf16 matrix cores with fp32 sums.  A code times its page's
-// power-of-two scale is a bf16 number (four significant bits), so K and V are
-// widened exactly, two codes an instruction, in operand order as they lie in the
-// cache.  (Scores on the fp8 matrix cores, the queries split in two e4m3 terms,
-// were 13% faster with many rows, but those instructions drop low bits of small
-// products, up to 1.3e-5 of a sum's magnitudes, which would be the error of lse;
-// probabilities split in two e4m3 terms cost more vector work than widening V.)
-// Probabilities are rounded to bf16 for the product with V, as in the sparse
-// forward; row sums take them unrounded, in fp32.
+// power-of-two scale is a bf16 number (four significant bits; scales below 2^-117
+// leave its normal range, far below any sum's rounding), so K and V are widened
+// exactly, two codes an instruction, in operand order as they lie in the cache.
+// (The fp8 matrix cores, with queries and probabilities split in two e4m3 terms,
+// were no faster, and drop low bits of small products: up to 1.3e-5 of a sum's
+// magnitudes, which would be the error of lse.)  Probabilities are rounded to
+// bf16 for the product with V, as in the sparse forward; row sums take them
+// unrounded, in fp32.
 //
 // A wave serves 32 rows (a row: one query head of one token; the heads that
 // share a key head are rows side by side).  Two kernels share that step:
