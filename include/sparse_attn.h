@@ -453,8 +453,8 @@ typedef struct {
  * over the tokens appended to it since its slot 0 was last written, the scale
  * is 2^e.  When a token raises e, the page's earlier codes are rounded to the
  * new scale (exact unless they become subnormal).  Slots behind a sequence's
- * last token keep their codes.  No page may be given to two sequences that get
- * tokens in it in one call.  Rows of q_out outside every sequence are left
+ * last token keep their codes.  No page may stand at two places of the tables
+ * that get tokens in one call.  Rows of q_out outside every sequence are left
  * as they are.  T == 0 launches nothing.
  * Errors: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED (head_dim, sizes beyond 32-bit
  * work items). */

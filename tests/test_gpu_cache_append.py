@@ -111,6 +111,19 @@ def test_many_sequences_of_one_token():
              q=tokens(B, 4, 3), what="batch")
 
 
+def test_thousands_of_sequences():
+    # found in three steps; many get no token
+    B = 5000
+    rng = np.random.default_rng(10)
+    new = rng.integers(0, 3, B)
+    start = np.concatenate([[0], np.cumsum(new)])
+    total = new + rng.integers(0, 62, B)
+    T = int(start[-1])
+    c = Cache(B, 1, rng.permutation(B).reshape(B, 1))
+    c.append(tokens(T, 1, 4), tokens(T, 1, 5), start, total, rope=table(64, 64), q=tokens(T, 1, 6),
+             what="5000 sequences")
+
+
 def test_token_by_token_with_growing_and_shrinking_tokens():
     c = Cache(3, 2, [[2, 0]])
     rng = np.random.default_rng(9)

@@ -134,6 +134,14 @@ def test_more_than_a_wave_of_sequences():
     run(lengths, [min(n, 1 + i % 2) for i, n in enumerate(lengths)], 1, 2)
 
 
+@pytest.mark.parametrize("B", [65, 4096, 5000])
+def test_thousands_of_sequences(B):
+    # found in one, two or three steps; a third of them get no token, some hold none
+    rng = np.random.default_rng(B)
+    lengths = rng.integers(0, 9, B).tolist()
+    run(lengths, [min(n, int(rng.integers(0, 3))) for n in lengths], 1, 1, 1, 0, front=1, back=2)
+
+
 @pytest.mark.parametrize("chunk,window", [(0, 0), (1, 0), (1, 130), (5, 3), (300, 1)])
 @pytest.mark.parametrize("g,most", [(3, 4), (8, 9), (1, 60)])
 def test_equal_shares_of_ragged_long_caches(g, most, chunk, window):
