@@ -677,27 +677,28 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
 }
 
 // ---- parts joined -------------------------------------------------------------
-// One wave per (token, head), two channels a lane.  The loads of the shares do
-// not wait for the sequence's own numbers: 16 at a time, what no part wrote
-// counting nothing.
+// W waves per (token, head), two channels a lane; each takes an equal run of the
+// parts, the first joins the runs.  The loads of the shares do not wait for the
+// sequence's own numbers: 16 at a time, what no part wrote counting nothing.
 constexpr int kJoin = 16;
-template <int R>
-__global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
-  const int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
-  const int lane = threadIdx.x & (kWave - 1);
+template <int R, int W>
+__global__ __launch_bounds__(W == 1 ? kThreads : W * kWave) void fwd_cache_join_kernel(Params p) {
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * kWaves + wave : (int64_t)blockIdx.x;
   if (row >= (int64_t)p.c.T * p.H) return;
+  const int run = (p.splits + W - 1) / W, first = W == 1 ? 0 : wave * run;  // run <= 64
+  const int mine = min(run, p.splits - first);                              // (none: <= 0)
   const int64_t step = (int64_t)p.c.T * p.H;
-  const float* from = p.part_o + row * kHeadDim + 2 * lane;
+  const float* from = p.part_o + (first * step + row) * kHeadDim + 2 * lane;
   float2 v[kJoin];
   auto fetch = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kJoin; ++i)
-      if (i0 + i < p.splits)
-        v[i] = *reinterpret_cast<const float2*>(from + (i0 + i) * step * kHeadDim);
+      if (i0 + i < mine) v[i] = *reinterpret_cast<const float2*>(from + (i0 + i) * step * kHeadDim);
   };
   fetch(0);
   float2 ml = make_float2(-INFINITY, 0.f);
-  if (lane < p.splits) ml = p.part_ml[lane * step + row];
+  if (lane < mine) ml = p.part_ml[(first + lane) * step + row];
   const int tok = (int)(row / p.H), head = (int)(row - (int64_t)tok * p.H);
   Tile t;
   t.b = find_sequence(p.c, tok, [](int s, int) { return s; }, &t.sp);
@@ -705,12 +706,13 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
   t.rows = t.sp.n * p.c.g;
   t.row0 = ((tok - t.sp.start) * p.c.g + head % p.c.g) / R * R;
   tile_range<R>(p.c, &t);
-  const int parts = parts_of(t.pages, p.splits, p.least);
-  if (parts == 1) return;  // written whole
+  const int all = parts_of(t.pages, p.splits, p.least);
+  if (all == 1) return;  // written whole
+  const int parts = min(all - first, mine);  // of this wave's run
   if (lane >= parts) ml = make_float2(-INFINITY, 0.f);
-  const float m = wave_max(ml.x);
+  float m = wave_max(ml.x);
   const float a = __builtin_amdgcn_exp2f(ml.x - (m == -INFINITY ? 0.f : m));
-  const float l = wave_sum_f32(a * ml.y);
+  float l = wave_sum_f32(a * ml.y);
   float x = 0.f, y = 0.f;
   for (int i0 = 0; i0 < parts; i0 += kJoin) {
     if (i0 > 0) fetch(i0);
@@ -722,6 +724,22 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
         y = fmaf(ai, v[i].y, y);
       }
   }
+  if constexpr (W > 1) {
+    __shared__ float2 sxy[W][kWave], sml[W];
+    sxy[wave][lane] = make_float2(x, y);
+    if (lane == 0) sml[wave] = make_float2(m, l);
+    __syncthreads();
+    if (wave != 0) return;
+    for (int i = 1; i < W; ++i) m = fmaxf(m, sml[i].x);
+    x = y = l = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float ai = __builtin_amdgcn_exp2f(sml[i].x - (m == -INFINITY ? 0.f : m));
+      l = fmaf(ai, sml[i].y, l);
+      x = fmaf(ai, sxy[i][lane].x, x);
+      y = fmaf(ai, sxy[i][lane].y, y);
+    }
+  }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   *reinterpret_cast<uint32_t*>(p.o + tok * p.o_tok + head * p.o_head + 2 * lane) =
       pack_bf16x2(x * inv, y * inv);
@@ -729,9 +747,11 @@ __global__ __launch_bounds__(kThreads) void fwd_cache_join_kernel(Params p) {
 }
 
 // How the work is cut.  Few rows a sequence go to the kernel that is bound by
-// the cache's bytes.  A part is given at least one page a wave where there are
-// not enough workgroups for every CU, four where there are (its start and end
-// cost about as much as two pages).
+// the cache's bytes.  Where its tiles do not fill the slots, a range is cut until
+// they do, or until there is one workgroup a CU where that leaves parts of fewer
+// than eight pages (a part's start and end cost about as much as two pages; one
+// token over 32,768 of 4 heads: 12.4 us, 16.7 with all slots filled); a part has
+// at least one page a wave, four where the tiles alone fill the slots.
 // Short tables are not cut: one token over 24 pages of 12 heads takes 13.0 us in
 // a stream of calls, 30 alone and 10.6 in a captured graph whole, 15.7, 29 and
 // 9.5 in parts; over 48 pages 16.5, 36 and 17, in parts 15.7, 30 and 9.8.
@@ -742,6 +762,7 @@ struct Plan {
   int splits, least;
 };
 constexpr int kSlots = 512;  // workgroups that run at once: 256 CUs, two each
+constexpr int kMostParts = kSlots;  // (joined by 8 waves of 64)
 Plan plan_of(const CacheIn& c) {
   Plan pl;
   const int64_t rows = (int64_t)c.T * c.g;
@@ -754,15 +775,30 @@ Plan plan_of(const CacheIn& c) {
     // run on alone
     pl.least = have >= kSlots ? 16 : 4;
     s = (8 * kSlots + have - 1) / have;
-    if (have < kSlots && s > (kSlots + have - 1) / have) s = (kSlots + have - 1) / have;
+    if (have < kSlots) {
+      s = (kSlots + have - 1) / have;
+      // parts of fewer than eight pages: one workgroup a CU
+      if (c.max_pages / s < 8) s = (kSlots / 2 + have - 1) / have;
+    }
   } else {
     pl.least = 8;
     s = have >= kSlots / 2 ? 1 : kSlots / have;
   }
   if (s > c.max_pages / pl.least) s = c.max_pages / pl.least;
   if (c.max_pages <= kWhole) s = 1;
-  pl.splits = (int)(s < 1 ? 1 : s > kWave ? kWave : s);
+  pl.splits = (int)(s < 1 ? 1 : s > kMostParts ? kMostParts : s);
   return pl;
+}
+
+template <int R>
+void join(const Params& p, hipStream_t stream) {
+  const unsigned rows = (unsigned)((int64_t)p.c.T * p.H);
+  if (p.splits <= kJoin)
+    fwd_cache_join_kernel<R, 1><<<(rows + kWaves - 1) / kWaves, kThreads, 0, stream>>>(p);
+  else if (p.splits <= 4 * kWave)
+    fwd_cache_join_kernel<R, 4><<<rows, 4 * kWave, 0, stream>>>(p);
+  else
+    fwd_cache_join_kernel<R, 8><<<rows, 8 * kWave, 0, stream>>>(p);
 }
 
 }  // namespace
@@ -798,11 +834,10 @@ hipError_t launch_fwd_cache(const FwdCacheIn& in, void* ws, hipStream_t stream) 
     fwd_cache_many_kernel<<<grid, kThreads, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.splits == 1) return e;
-  const unsigned rows = (unsigned)(((int64_t)in.c.T * p.H + kWaves - 1) / kWaves);
   if (pl.few)
-    fwd_cache_join_kernel<kFewRows><<<rows, kThreads, 0, stream>>>(p);
+    join<kFewRows>(p, stream);
   else
-    fwd_cache_join_kernel<kManyRows><<<rows, kThreads, 0, stream>>>(p);
+    join<kManyRows>(p, stream);
   return hipGetLastError();
 }
 

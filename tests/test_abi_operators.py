@@ -206,9 +206,10 @@ def test_fwd_cache_workspace():
     assert size() >= 16 and size(tokens=0) >= 16
     assert size(tokens=1 << 25) > 0 and size(tokens=(1 << 25) + 1) == 0
     assert size(batch=1 << 19) > 0 and size(batch=(1 << 19) + 1) == 0
-    # parts are bounded: one long sequence, 64 of them
-    one = size(batch=1, tokens=1, max_pages=1 << 20, pages_stride=1 << 20)
-    assert one == 64 * 8 * (128 * 4 + 8)
+    # parts are bounded: one long sequence, 512 workgroups
+    long = dict(batch=1, tokens=1, max_pages=1 << 20, pages_stride=1 << 20)
+    assert size(**long) == 512 // 4 * 8 * (128 * 4 + 8)
+    assert size(**long, kv_heads=1) == 512 * 8 * (128 * 4 + 8)
 
 
 @pytest.mark.parametrize("bad", BAD_CACHE_TENSORS + [

@@ -159,6 +159,12 @@ def test_one_long_sequence_in_many_parts(kv):
     run([64, 9000, 1], [1, 3, 1], kv, 2, 1, 0, seed=6)
 
 
+def test_parts_beyond_a_wave_of_them():
+    run([70000], [1], 1, 64, seed=7)                     # 64 rows: the many-row kernel, 136 parts
+    run([262144 + 100], [1], 1, 2, seed=8)               # 512 parts
+    run([30000, 0, 5], [2, 0, 1], 1, 8, 1, 20000, seed=9)  # 117 parts at most, a window of 20,000
+
+
 def test_large_scores_and_a_late_maximum():
     # logits spread over hundreds: later pages move the maximum far, most
     # probabilities vanish
