@@ -512,8 +512,8 @@ enum { SA_BF16 = 0, SA_F32 = 1 };
  *  weight, bias  fp32 [groups][cols], or NULL for ones and zeros
  *  eps     >= 0
  *  mean, rstd    fp32 [rows] out, or NULL
- * Rows of whole 16-byte aligned pieces (cols % 8 == 0, x and y 16-byte aligned
- * with row strides of whole 16 bytes) move 16 bytes a load; others an element.
+ * Rows move in 16-byte pieces from any aligned element; bf16 rows that start at
+ * odd elements take up to a third longer.
  * Errors: SA_ERR_INVALID_ARG; SA_ERR_UNSUPPORTED beyond the limits above. */
 int sparse_attn_layer_norm(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols,
                            int64_t groups, const float* weight, const float* bias, float eps,

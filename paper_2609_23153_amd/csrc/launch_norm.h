@@ -32,7 +32,7 @@ struct LayerNormBwdIn {
   bool f32;
 };
 hipError_t launch_layer_norm(const LayerNormIn& in, hipStream_t stream);
-// Workspace: the teams' partial weight gradients, fp32 [groups][teams][2][cols].
+// Workspace: the workgroups' partial weight gradients, fp32 [groups][workgroups][2][cols].
 size_t layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols, int64_t groups);
 hipError_t launch_layer_norm_bwd(const LayerNormBwdIn& in, void* ws, hipStream_t stream);
 

@@ -5,12 +5,12 @@
 //   dx = rstd (g - mean(g) - xh mean(g xh)),  dw = sum_rows dy xh,  db = sum_rows dy
 //
 // Rows form groups of equal size, each with its own weight and bias (a video
-// DiT modulates the norm per sample).  A team of 64 or 256 threads keeps a
+// DiT modulates the norm per sample).  A team of 16 to 512 threads keeps a
 // row in registers, so every tensor moves once; it walks rows of its group
 // with the weights (backward: and its share of dw, db) in registers and the
 // next row's loads in flight.  Every statistic and sum is fp32.  The weights'
-// gradients leave a team as one partial row each, which a second kernel adds
-// in a fixed order: no atomics, the same bits every time.
+// gradients leave a workgroup as one partial row each, which a second kernel
+// adds in a fixed order: no atomics, the same bits every time.
 #include <type_traits>
 
 #include "launch_norm.h"
@@ -19,19 +19,45 @@
 namespace sa {
 namespace {
 
-constexpr int kMaxTeamWaves = 4;
-
-// 16 bytes; ONCE: data too large for the caches, which it is then kept out of.
-template <bool ONCE>
-__device__ __forceinline__ u32x4 piece_ld(const void* p) {
-  return ONCE ? ld16_once(p) : ld16(p);
+// 16 bytes at any element's address; ONCE: data too large for the caches, which
+// it is then kept out of.
+template <typename T>
+struct Any16;
+template <>
+struct Any16<uint16_t> {
+  typedef u32x4 type __attribute__((aligned(2)));
+};
+template <>
+struct Any16<float> {
+  typedef u32x4 type __attribute__((aligned(4)));
+};
+template <bool ONCE, typename T>
+__device__ __forceinline__ u32x4 piece_ld(const T* p) {
+  typedef typename Any16<T>::type V;
+  return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const V*>(p))
+              : *reinterpret_cast<const V*>(p);
 }
-template <bool ONCE>
-__device__ __forceinline__ void piece_st(void* p, u32x4 v) {
+template <bool ONCE, typename T>
+__device__ __forceinline__ void piece_st(T* p, u32x4 v) {
+  typedef typename Any16<T>::type V;
   if (ONCE)
-    __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+    __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
   else
-    st16(p, v);
+    *reinterpret_cast<V*>(p) = v;
+}
+
+// x summed over a team's lanes of one wave (16 of them, or all 64).
+template <int TPR>
+__device__ __forceinline__ float team_sum(float x) {
+  return TPR < kWave ? row_sum_f32(x) : wave_sum_f32(x);
+}
+
+// The thread's team of its workgroup's; uniform in a wave where it can be.
+template <int TPR, int TEAMS>
+__device__ __forceinline__ int team_index() {
+  if (TEAMS == 1) return 0;
+  const int i = threadIdx.x / TPR;
+  return TPR < kWave ? i : __builtin_amdgcn_readfirstlane(i);
 }
 
 // VEC consecutive elements of a row as loaded, and their fp32 values.
@@ -86,25 +112,41 @@ struct Piece<float, 1, false> {
   static __device__ __forceinline__ void store(float* p, const float* v) { *p = v[0]; }
 };
 
-// fp32 weights at columns c .. c + VEC - 1 (`none` where there are none).
+// Columns of a thread's k-th piece: it owns those from c on, and holds the VEC from
+// `at` on.  At the row's end `at` is less than c where the row is not made of whole
+// pieces (WHOLE): the piece then holds columns of the one before as well, of which
+// it writes the same values; past the end it owns none (and holds the last ones: a
+// branch around the load would keep the last row's pieces alive).
+template <int VEC, bool WHOLE>
+struct Columns {
+  int c, at;
+  bool some;  // owns any
+  __device__ __forceinline__ Columns(int c, int cols)
+      : c(c), at(min(c, cols - VEC)), some(c < cols) {}
+  __device__ __forceinline__ bool owns(int e) const { return WHOLE ? some : at + e >= c; }
+};
+
+// fp32 weights of the thread's pieces (`none` where there are none).
 template <int VEC, int NC, int TPR>
 __device__ __forceinline__ void load_weights(float (&w)[NC][VEC], const float* p, int cols,
                                              float none) {
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    const int c = ((int)threadIdx.x + TPR * k) * VEC;
+    const int at = min(((int)threadIdx.x % TPR + TPR * k) * VEC, cols - VEC);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) w[k][e] = p && c < cols ? p[c + e] : none;
+    for (int e = 0; e < VEC; ++e) w[k][e] = p ? p[at + e] : none;
   }
 }
 
-template <typename T, int VEC, bool ONCE, int TPR, int NC>
-__global__ __launch_bounds__(TPR) void layer_norm_kernel(
+template <typename T, int VEC, bool WHOLE, bool ONCE, int TPR, int NC>
+__global__ __launch_bounds__(TPR < kWave ? kWave : TPR) void layer_norm_kernel(
     const T* x, int64_t ldx, int64_t rows, int cols, const float* weight, const float* bias,
     float eps, T* y, int64_t ldy, float* mean_out, float* rstd_out) {
   using P = Piece<T, VEC, ONCE>;
-  constexpr int kWaves = TPR / kWave;
-  const int tid = threadIdx.x, wave = tid / kWave;
+  using Cols = Columns<VEC, WHOLE>;
+  constexpr int kWaves = TPR < kWave ? 1 : TPR / kWave;  // of a team
+  constexpr int kTeams = TPR < kWave ? kWave / TPR : 1;  // of a workgroup
+  const int tid = threadIdx.x % TPR, wave = tid / kWave;
   const int64_t first = (int64_t)blockIdx.y * rows;  // first row of the group
   float w[NC][VEC], b[NC][VEC];
   load_weights<VEC, NC, TPR>(w, weight ? weight + (int64_t)blockIdx.y * cols : nullptr, cols, 1.f);
@@ -116,46 +158,48 @@ __global__ __launch_bounds__(TPR) void layer_norm_kernel(
     int n = 0;
 #pragma unroll
     for (int k = 0; k < NC; ++k)
-      n += min(max(cols - (v * kWave + TPR * k) * VEC, 0), kWave * VEC);
+      n += min(max(cols - (v * kWave + TPR * k) * VEC, 0), TPR / kWaves * VEC);
     nw[v] = (float)n;
   }
-  __shared__ float2 red[2][kMaxTeamWaves];
+  __shared__ float2 red[2][kWaves];
 
   P next[NC];
   auto fetch = [&](int64_t r) __attribute__((always_inline)) {
+    const T* xr = x + (first + r) * ldx;
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = (tid + TPR * k) * VEC;
-      if (c < cols) next[k].load(x + (first + r) * ldx + c);
-    }
+    for (int k = 0; k < NC; ++k) next[k].load(xr + Cols((tid + TPR * k) * VEC, cols).at);
   };
-  int64_t r = blockIdx.x;
+  int64_t r = (int64_t)blockIdx.x * kTeams + team_index<TPR, kTeams>();
   if (r < rows) fetch(r);
   for (int turn = 0; r < rows; turn ^= 1) {
     float v[NC][VEC];
     float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < NC; ++k)
+    for (int k = 0; k < NC; ++k) {
+      const Cols c((tid + TPR * k) * VEC, cols);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        v[k][e] = (tid + TPR * k) * VEC < cols ? next[k].get(e) : 0.f;
-        s += v[k][e];
+        v[k][e] = next[k].get(e);
+        s += c.owns(e) ? v[k][e] : 0.f;
       }
+    }
     const int64_t row = first + r;
-    r += gridDim.x;
+    r += (int64_t)gridDim.x * kTeams;
     if (r < rows) fetch(r);
     // mean and squared deviations of the wave's elements, then of the row:
     // deviations are taken from a mean, never as a difference of squares
-    const float mw = nw[wave] > 0.f ? wave_sum_f32(s) / nw[wave] : 0.f;
+    const float mw = nw[wave] > 0.f ? team_sum<TPR>(s) / nw[wave] : 0.f;
     float d2 = 0.f;
 #pragma unroll
-    for (int k = 0; k < NC; ++k)
+    for (int k = 0; k < NC; ++k) {
+      const Cols c((tid + TPR * k) * VEC, cols);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float d = (tid + TPR * k) * VEC < cols ? v[k][e] - mw : 0.f;
+        const float d = c.owns(e) ? v[k][e] - mw : 0.f;
         d2 = fmaf(d, d, d2);
       }
-    d2 = wave_sum_f32(d2);
+    }
+    d2 = team_sum<TPR>(d2);
     float mean = mw, m2 = d2;
     if constexpr (kWaves > 1) {
       if ((tid & (kWave - 1)) == 0) red[turn][wave] = make_float2(mw, d2);
@@ -172,13 +216,14 @@ __global__ __launch_bounds__(TPR) void layer_norm_kernel(
       }
     }
     const float rstd = 1.f / sqrtf(m2 / (float)cols + eps);
+    T* yr = y + row * ldy;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int c = (tid + TPR * k) * VEC;
+      const Cols c((tid + TPR * k) * VEC, cols);
       float o[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) o[e] = fmaf((v[k][e] - mean) * rstd, w[k][e], b[k][e]);
-      if (c < cols) P::store(y + row * ldy + c, o);
+      if (c.some) P::store(yr + c.at, o);
     }
     if (tid == 0) {
       if (mean_out) mean_out[row] = mean;
@@ -187,13 +232,20 @@ __global__ __launch_bounds__(TPR) void layer_norm_kernel(
   }
 }
 
-template <typename T, int VEC, bool ONCE, int TPR, int NC>
-__global__ __launch_bounds__(TPR) void layer_norm_bwd_kernel(
+constexpr int kBwdThreads = 256;  // of a workgroup at least: teams of fewer threads share one
+template <typename T, int VEC, bool WHOLE, bool ONCE, int TPR, int NC>
+__global__ __launch_bounds__(TPR < kBwdThreads ? kBwdThreads : TPR) void layer_norm_bwd_kernel(
     const T* dy, int64_t lddy, const T* x, int64_t ldx, const float* mean, const float* rstd,
     int64_t rows, int cols, const float* weight, T* dx, int64_t lddx, float* part) {
   using P = Piece<T, VEC, ONCE>;
-  constexpr int kWaves = TPR / kWave;
-  const int tid = threadIdx.x, wave = tid / kWave;
+  using Cols = Columns<VEC, WHOLE>;
+  constexpr int kWaves = TPR < kWave ? 1 : TPR / kWave;              // of a team
+  constexpr int kTeams = TPR < kBwdThreads ? kBwdThreads / TPR : 1;  // of a workgroup
+  static_assert(kTeams == 1 || kWaves == 1, "teams that share a workgroup have no barriers");
+  // The longest rows hide their loads among themselves, and have no registers for
+  // the next one's.
+  constexpr bool kAhead = TPR <= 512;
+  const int tid = threadIdx.x % TPR, wave = tid / kWave;
   const int64_t first = (int64_t)blockIdx.y * rows;
   float w[NC][VEC], dw[NC][VEC], db[NC][VEC];
   load_weights<VEC, NC, TPR>(w, weight ? weight + (int64_t)blockIdx.y * cols : nullptr, cols, 1.f);
@@ -201,7 +253,7 @@ __global__ __launch_bounds__(TPR) void layer_norm_bwd_kernel(
   for (int k = 0; k < NC; ++k)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) dw[k][e] = db[k][e] = 0.f;
-  __shared__ float2 red[2][kMaxTeamWaves];
+  __shared__ float2 red[2][kWaves];
   const float inv = 1.f / (float)cols;
 
   P nx[NC], ny[NC];
@@ -209,39 +261,41 @@ __global__ __launch_bounds__(TPR) void layer_norm_bwd_kernel(
   auto fetch = [&](int64_t r) __attribute__((always_inline)) {
     nm = mean[first + r];
     nr = rstd[first + r];
+    const T *xr = x + (first + r) * ldx, *yr = dy + (first + r) * lddy;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int c = (tid + TPR * k) * VEC;
-      if (c < cols) {
-        nx[k].load(x + (first + r) * ldx + c);
-        ny[k].load(dy + (first + r) * lddy + c);
-      }
+      const Cols c((tid + TPR * k) * VEC, cols);
+      nx[k].load(xr + c.at);
+      ny[k].load(yr + c.at);
     }
   };
-  int64_t r = blockIdx.x;
-  if (r < rows) fetch(r);
+  int64_t r = (int64_t)blockIdx.x * kTeams + team_index<TPR, kTeams>();
+  if (kAhead && r < rows) fetch(r);
   for (int turn = 0; r < rows; turn ^= 1) {
+    if (!kAhead) fetch(r);
     float xh[NC][VEC], g[NC][VEC];
     float sg = 0.f, sx = 0.f;
     const float rs = nr;
 #pragma unroll
-    for (int k = 0; k < NC; ++k)
+    for (int k = 0; k < NC; ++k) {
+      const Cols c((tid + TPR * k) * VEC, cols);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const bool in = (tid + TPR * k) * VEC < cols;
-        xh[k][e] = in ? (nx[k].get(e) - nm) * rs : 0.f;
-        const float d = in ? ny[k].get(e) : 0.f;
+        xh[k][e] = (nx[k].get(e) - nm) * rs;
+        const float d = ny[k].get(e);
         dw[k][e] = fmaf(d, xh[k][e], dw[k][e]);
         db[k][e] += d;
         g[k][e] = d * w[k][e];
-        sg += g[k][e];
-        sx = fmaf(g[k][e], xh[k][e], sx);
+        const float mine = c.owns(e) ? g[k][e] : 0.f;
+        sg += mine;
+        sx = fmaf(mine, xh[k][e], sx);
       }
+    }
     const int64_t row = first + r;
-    r += gridDim.x;
-    if (r < rows) fetch(r);
-    sg = wave_sum_f32(sg);
-    sx = wave_sum_f32(sx);
+    r += (int64_t)gridDim.x * kTeams;
+    if (kAhead && r < rows) fetch(r);
+    sg = team_sum<TPR>(sg);
+    sx = team_sum<TPR>(sx);
     if constexpr (kWaves > 1) {
       if ((tid & (kWave - 1)) == 0) red[turn][wave] = make_float2(sg, sx);
       __syncthreads();
@@ -254,46 +308,71 @@ __global__ __launch_bounds__(TPR) void layer_norm_bwd_kernel(
     }
     sg *= inv;
     sx *= inv;
+    T* xr = dx + row * lddx;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int c = (tid + TPR * k) * VEC;
+      const Cols c((tid + TPR * k) * VEC, cols);
       float o[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) o[e] = (g[k][e] - sg - xh[k][e] * sx) * rs;
-      if (c < cols) P::store(dx + row * lddx + c, o);
+      if (c.some) P::store(xr + c.at, o);
     }
   }
-  if (part) {
-    float* p = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * cols;
+  if (!part) return;
+  float* p = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * cols;
+  if constexpr (kTeams > 1) {  // the workgroup's teams: those of a wave, then the waves
+    constexpr int kBlockWaves = kBwdThreads / kWave;
+    __shared__ float all[kBlockWaves][2][NC * TPR * VEC];
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int c = (tid + TPR * k) * VEC;
-      if (c < cols) {
+      const Cols c((tid + TPR * k) * VEC, cols);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          p[c + e] = dw[k][e];
-          p[cols + c + e] = db[k][e];
+      for (int e = 0; e < VEC; ++e) {
+        const float a = TPR < kWave ? across_rows_f32(dw[k][e]) : dw[k][e];
+        const float b = TPR < kWave ? across_rows_f32(db[k][e]) : db[k][e];
+        if (c.owns(e)) {  // (a wave's teams alike)
+          all[threadIdx.x / kWave][0][c.at + e] = a;
+          all[threadIdx.x / kWave][1][c.at + e] = b;
         }
       }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * cols; c += kBwdThreads) {
+      const int which = c < cols ? 0 : 1, at = c - which * cols;
+      float v = 0.f;
+#pragma unroll
+      for (int i = 0; i < kBlockWaves; ++i) v += all[i][which][at];
+      p[c] = v;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      const Cols c((tid + TPR * k) * VEC, cols);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (c.owns(e)) {
+          p[c.at + e] = dw[k][e];
+          p[cols + c.at + e] = db[k][e];
+        }
     }
   }
 }
 
-// dw, db of a group: the teams' partial rows added in a fixed order, 64
-// columns a workgroup, 16 runs of teams side by side.
+// dw, db of a group: the workgroups' partial rows added in a fixed order, 64
+// columns a workgroup, 16 runs of them side by side.
 constexpr int kRedRuns = 16;
 __global__ __launch_bounds__(kWave* kRedRuns) void layer_norm_reduce_kernel(const float* part,
-                                                                           int teams, int cols,
+                                                                           int parts, int cols,
                                                                            float* dw, float* db) {
   __shared__ float s[kRedRuns][kWave];
   const int lane = threadIdx.x & (kWave - 1), run = threadIdx.x / kWave;
   const int which = blockIdx.x & 1, c = (int)(blockIdx.x >> 1) * kWave + lane;
   float* out = which ? db : dw;
-  const float* p = part + ((int64_t)blockIdx.y * teams * 2 + which) * cols;
+  const float* p = part + ((int64_t)blockIdx.y * parts * 2 + which) * cols;
   float sum = 0.f;
   if (c < cols) {
-#pragma unroll 8
-    for (int t = run; t < teams; t += kRedRuns) sum += p[(int64_t)t * 2 * cols + c];
+#pragma unroll 16
+    for (int t = run; t < parts; t += kRedRuns) sum += p[(int64_t)t * 2 * cols + c];
   }
   s[run][lane] = sum;
   __syncthreads();
@@ -305,120 +384,133 @@ __global__ __launch_bounds__(kWave* kRedRuns) void layer_norm_reduce_kernel(cons
   }
 }
 
-// Threads per row, and the elements each holds at most.  Forward: a wave alone
-// needs no barrier and serves rows up to 2048 channels; longer ones take four.
-// Backward: four from 512 channels on, so that fewer teams, and with them fewer
-// partial gradients, keep as many waves busy (1,554 x 1,531 fp32: 777 one-wave
-// teams a group 26 us with the sum of the partials, 128 of four waves 18.5).
-struct Team {
-  int threads, elems;
-};
-Team team_of(int64_t cols, bool backward) {
-  if (cols <= 512) return {64, 8};
-  if (cols <= 2048) return backward ? Team{256, 8} : Team{64, 32};
-  if (cols <= 6144) return {256, 24};
-  return {256, 64};
+// Threads per row.  Up to 128 channels, four rows share a wave (75,600 x 96 bf16:
+// 14 us, a wave a row 26).  Forward: a wave alone needs no barrier and serves rows
+// up to 2048 channels; longer ones take four or eight.  Backward: four from 1024
+// channels on, so that fewer workgroups, and with them fewer partial gradients,
+// keep as many waves busy (1,554 x 1,531 fp32: 777 one-wave teams a group 26 us
+// with the sum of the partials, 128 of four waves 18.5); eight from 6144 on, as a
+// thread of four would hold more than 24 elements and spill (20,000 x 9,000 bf16:
+// 308 us, 244 with eight); sixteen from 12288 on, without the next row's loads in
+// flight (6,000 x 16,384 fp32: eight 450 us, sixteen 296).
+int team_of(int64_t cols, bool backward) {
+  if (cols <= 128) return 16;
+  if (cols <= 1024) return 64;
+  if (cols <= 2048) return backward ? 256 : 64;
+  if (cols <= 6144) return 256;
+  return cols <= 12288 || !backward ? 512 : 1024;
 }
 
-int fwd_teams(int64_t rows, int64_t cols, int64_t groups) {
-  const int64_t cap = (team_of(cols, false).threads == 64 ? 8192 : 2048) / groups;
-  return (int)(rows < cap ? rows : cap < 1 ? 1 : cap);
+// Workgroups of a group of `rows` rows, forward: as many as run at once.
+int fwd_blocks(int64_t rows, int64_t cols, int64_t groups) {
+  const int team = team_of(cols, false), teams = team < kWave ? kWave / team : 1;
+  const int64_t cap = (team <= 64 ? 8192 : 524288 / team) / groups, most = (rows + teams - 1) / teams;
+  return (int)(most < cap ? most : cap < 1 ? 1 : cap);
 }
-// Teams of a group of `rows` rows: each adds a partial row of 2 x cols floats to
-// write and read, so none has fewer than 8 rows while 256 teams are there.
-int bwd_teams(int64_t rows, int64_t cols, int64_t groups) {
-  const int64_t most = team_of(cols, true).threads == 64 ? 2048 : 1024;
+// Backward: each adds a partial row of 2 x cols floats to write and read, so none
+// has fewer than 8 rows while 256 of them are there.
+int bwd_blocks(int64_t rows, int64_t cols, int64_t groups) {
+  const int team = team_of(cols, true), teams = team < kBwdThreads ? kBwdThreads / team : 1;
+  const int64_t most = (rows + teams - 1) / teams;
   int64_t t = rows * groups / 8;
-  t = (t < 256 ? 256 : t > most ? most : t) / groups;
-  t = t < rows ? t : rows;
+  t = (t < 256 ? 256 : t > 1024 ? 1024 : t) / groups;
+  t = t < most ? t : most;
   return (int)(t < 1 ? 1 : t);
 }
 
-template <typename T, int VEC, bool ONCE, int TPR, int NC>
+template <typename T, int VEC, bool WHOLE, bool ONCE, int TPR, int NC>
 void run(const LayerNormIn& in, float*, hipStream_t stream) {
   const int64_t per = in.rows / in.groups;
-  const dim3 grid(fwd_teams(per, in.cols, in.groups), (unsigned)in.groups);
-  layer_norm_kernel<T, VEC, ONCE, TPR, NC><<<grid, TPR, 0, stream>>>(
+  const dim3 grid(fwd_blocks(per, in.cols, in.groups), (unsigned)in.groups);
+  layer_norm_kernel<T, VEC, WHOLE, ONCE, TPR, NC><<<grid, TPR < kWave ? kWave : TPR, 0, stream>>>(
       static_cast<const T*>(in.x), in.ldx, per, (int)in.cols, in.weight, in.bias, in.eps,
       static_cast<T*>(in.y), in.ldy, in.mean, in.rstd);
 }
-template <typename T, int VEC, bool ONCE, int TPR, int NC>
+template <typename T, int VEC, bool WHOLE, bool ONCE, int TPR, int NC>
 void run(const LayerNormBwdIn& in, float* part, hipStream_t stream) {
   const int64_t per = in.rows / in.groups;
-  const dim3 grid(bwd_teams(per, in.cols, in.groups), (unsigned)in.groups);
-  layer_norm_bwd_kernel<T, VEC, ONCE, TPR, NC><<<grid, TPR, 0, stream>>>(
-      static_cast<const T*>(in.dy), in.lddy, static_cast<const T*>(in.x), in.ldx, in.mean, in.rstd,
-      per, (int)in.cols, in.weight, static_cast<T*>(in.dx), in.lddx, part);
+  const dim3 grid(bwd_blocks(per, in.cols, in.groups), (unsigned)in.groups);
+  layer_norm_bwd_kernel<T, VEC, WHOLE, ONCE, TPR, NC>
+      <<<grid, TPR < kBwdThreads ? kBwdThreads : TPR, 0, stream>>>(
+          static_cast<const T*>(in.dy), in.lddy, static_cast<const T*>(in.x), in.ldx, in.mean,
+          in.rstd, per, (int)in.cols, in.weight, static_cast<T*>(in.dx), in.lddx, part);
 }
 
-// The kernel for the row's length.
-template <typename T, int VEC, bool ONCE, typename In>
+// The kernel for the row's length (8 channels at least).
+template <typename T, bool WHOLE, bool ONCE, typename In>
 void run_team(const In& in, float* part, hipStream_t stream) {
   constexpr bool kBack = std::is_same<In, LayerNormBwdIn>::value;
-  const Team tm = team_of(in.cols, kBack);
-  if (in.cols <= 512)
-    run<T, VEC, ONCE, 64, 8 / VEC>(in, part, stream);
-  else if (in.cols <= 2048)
-    run<T, VEC, ONCE, kBack ? 256 : 64, (kBack ? 8 : 32) / VEC>(in, part, stream);
-  else if (tm.elems == 24)
-    run<T, VEC, ONCE, 256, 24 / VEC>(in, part, stream);
-  else
-    run<T, VEC, ONCE, 256, 64 / VEC>(in, part, stream);
+  switch (team_of(in.cols, kBack)) {
+    case 16:
+      return run<T, 8, WHOLE, ONCE, 16, 1>(in, part, stream);
+    case 64:
+      if (in.cols <= 512) return run<T, 8, WHOLE, ONCE, 64, 1>(in, part, stream);
+      if (kBack || in.cols <= 1024) return run<T, 8, WHOLE, ONCE, 64, 2>(in, part, stream);
+      if constexpr (!kBack) run<T, 8, WHOLE, ONCE, 64, 4>(in, part, stream);
+      return;
+    case 256:
+      if constexpr (kBack)
+        if (in.cols <= 2048) return run<T, 8, WHOLE, ONCE, 256, 1>(in, part, stream);
+      if (in.cols <= 4096) return run<T, 8, WHOLE, ONCE, 256, 2>(in, part, stream);
+      return run<T, 8, WHOLE, ONCE, 256, 3>(in, part, stream);
+    case 512:
+      if (kBack || in.cols <= 12288) return run<T, 8, WHOLE, ONCE, 512, 3>(in, part, stream);
+      if constexpr (!kBack) run<T, 8, WHOLE, ONCE, 512, 4>(in, part, stream);
+      return;
+    default:
+      if constexpr (kBack) run<T, 8, WHOLE, ONCE, 1024, 2>(in, part, stream);
+  }
 }
-// Rows of whole, aligned 16-byte pieces are moved by them (vec), others by
-// element.  More than twice what the last-level cache holds (256 MB) is kept
-// out of the caches (75,600 x 5,120 bf16: forward 321 -> 301 us, backward 460
-// -> 417); less is left in them, mostly for the call that reads the result
-// (4,680 rows: 19.5 us, kept out 22.6).
+// Rows move by pieces of eight elements from wherever they start: misaligned bf16
+// rows lose up to a third (40,000 x 5,119: forward 185 us, backward 308; 5,120: 154
+// and 232), fp32 rows nothing.  An element a load was slower for most (75,600 x 701
+// forward 71 us, 46 by pieces; 20,000 x 9,001 backward 496, 308), 10% faster for the
+// backward of some (5,119: 279).  More than twice
+// what the last-level cache holds (256 MB) is kept out of the caches (75,600 x
+// 5,120 bf16: forward 321 -> 301 us, backward 460 -> 417); less is left in them,
+// mostly for the call that reads the result (4,680 rows: 19.5 us, kept out 22.6).
 template <typename T, typename In>
-void run_rows(const In& in, float* part, bool vec, int tensors, hipStream_t stream) {
+void run_rows(const In& in, float* part, int tensors, hipStream_t stream) {
   const bool once = in.rows * in.cols * tensors * (int64_t)sizeof(T) > ((int64_t)512 << 20);
-  if (vec && once)
-    run_team<T, 8, true>(in, part, stream);
-  else if (vec)
-    run_team<T, 8, false>(in, part, stream);
+  if (in.cols < 8)
+    run<T, 1, true, false, 16, 1>(in, part, stream);
+  else if (in.cols % 8 != 0)
+    run_team<T, false, false>(in, part, stream);
+  else if (once)
+    run_team<T, true, true>(in, part, stream);
   else
-    run_team<T, 1, false>(in, part, stream);
-}
-
-bool whole(const void* p, int64_t ld, int elem) {  // 16-byte pieces stay aligned in every row
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * elem & 15) == 0;
+    run_team<T, true, false>(in, part, stream);
 }
 
 }  // namespace
 
 size_t layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols, int64_t groups) {
-  return (size_t)groups * bwd_teams(rows / groups, cols, groups) * 2 * cols * sizeof(float);
+  return (size_t)groups * bwd_blocks(rows / groups, cols, groups) * 2 * cols * sizeof(float);
 }
 
 hipError_t launch_layer_norm(const LayerNormIn& in, hipStream_t stream) {
   if (in.rows == 0) return hipSuccess;
-  const int elem = in.f32 ? 4 : 2;
-  const bool vec = in.cols % 8 == 0 && whole(in.x, in.ldx, elem) && whole(in.y, in.ldy, elem);
   if (in.f32)
-    run_rows<float>(in, nullptr, vec, 2, stream);
+    run_rows<float>(in, nullptr, 2, stream);
   else
-    run_rows<uint16_t>(in, nullptr, vec, 2, stream);
+    run_rows<uint16_t>(in, nullptr, 2, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_layer_norm_bwd(const LayerNormBwdIn& in, void* ws, hipStream_t stream) {
-  const int elem = in.f32 ? 4 : 2;
   float* part = in.dweight || in.dbias ? static_cast<float*>(ws) : nullptr;
   if (in.rows > 0) {
-    const bool vec = in.cols % 8 == 0 && whole(in.x, in.ldx, elem) &&
-                     whole(in.dy, in.lddy, elem) && whole(in.dx, in.lddx, elem);
     if (in.f32)
-      run_rows<float>(in, part, vec, 3, stream);
+      run_rows<float>(in, part, 3, stream);
     else
-      run_rows<uint16_t>(in, part, vec, 3, stream);
+      run_rows<uint16_t>(in, part, 3, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (part) {
-    const int teams = in.rows > 0 ? bwd_teams(in.rows / in.groups, in.cols, in.groups) : 0;
+    const int parts = in.rows > 0 ? bwd_blocks(in.rows / in.groups, in.cols, in.groups) : 0;
     const dim3 grid(2 * (unsigned)((in.cols + kWave - 1) / kWave), (unsigned)in.groups);
-    layer_norm_reduce_kernel<<<grid, kWave * kRedRuns, 0, stream>>>(part, teams, (int)in.cols,
+    layer_norm_reduce_kernel<<<grid, kWave * kRedRuns, 0, stream>>>(part, parts, (int)in.cols,
                                                                     in.dweight, in.dbias);
   }
   return hipGetLastError();

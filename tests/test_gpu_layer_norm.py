@@ -56,7 +56,8 @@ def near(got, want, scale, what):
 
 SHAPES = [(1, 1), (1, 8), (3, 7), (5, 64), (7, 511), (4, 512), (9, 513), (64, 1536), (33, 1531),
           (6, 2048), (10, 2049), (12, 5120), (5, 6144), (6, 6145), (3, 8960), (2, 16384), (3, 16383),
-          (3000, 96)]
+          (3000, 96), (50, 9), (700, 15), (21, 127), (40, 128), (17, 129), (9, 1023), (9, 1025),
+          (10, 4095), (5, 4097), (4, 12287), (4, 12288), (3, 12289), (5000, 100)]
 
 
 def check(rows, cols, dtype, groups, pad=0, eps=1e-6, shift=0.3):
@@ -106,6 +107,34 @@ def test_shapes(rows, cols, dtype):
                                                   (2, 4 * 1024 + 2, 2056, 0)])
 def test_groups_strides_and_long_walks(groups, rows, cols, pad, dtype):
     check(rows, cols, dtype, groups, pad)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [1, 7, 8, 9, 64, 125, 700, 1531, 4099, 9001, 12300])
+def test_rows_that_start_at_odd_elements(cols, dtype):
+    # one column in from an aligned buffer, with strides that keep no row aligned:
+    # the same bytes as for the same rows side by side, the columns around untouched
+    rows, pad = 70, 3
+    g = torch.Generator().manual_seed(cols)
+    x, dy = (torch.randn(rows, cols, generator=g).to(dtype).to(DEV) for _ in range(2))
+    w, b = (torch.randn(2, cols, generator=g).to(DEV) for _ in range(2))
+
+    def shifted(t):
+        buf = torch.full((rows, cols + pad), 7.0, dtype=dtype, device=DEV)
+        buf[:, 1:cols + 1] = t
+        return buf, buf[:, 1:cols + 1]
+
+    y, mean, rstd = sa.sparse_attn_layer_norm(x, w, b)
+    dx, dw, db = sa.sparse_attn_layer_norm_bwd(dy, x, mean, rstd, w)
+    xb, xs = shifted(x)
+    db_, ds = shifted(dy)
+    got = sa.sparse_attn_layer_norm_bwd(ds, xs, mean, rstd, w, dx=ds)        # in place
+    for a, c in zip(got, (dx, dw, db)):
+        assert torch.equal(a, c)
+    out, m, r = sa.sparse_attn_layer_norm(xs, w, b, y=xs)
+    assert torch.equal(out, y) and torch.equal(m, mean) and torch.equal(r, rstd)
+    for buf in (xb, db_):
+        assert bool((buf[:, 0] == 7.0).all()) and bool((buf[:, cols + 1:] == 7.0).all())
 
 
 def test_large_mean_keeps_the_variance():
