@@ -8,12 +8,11 @@
 // new token needs a larger one; then its old codes move to the new scale,
 // which is exact but for codes that become subnormal.
 //
-// One workgroup per page that gets tokens and key head for K, one for V, one
-// for the queries that share the key head: each tile has one writer, so nothing
-// races.  Bound by memory and, for few tokens, by the latency of dependent loads
-// (sequence, page, scale): three workgroups side by side take 4.5 us for one
-// token where one doing all took 5.8 (4,680 tokens of 12 heads, 72 MB: 19.9 us,
-// 18.8).
+// One workgroup per page that gets tokens and key head for K, one for V, one or
+// more for the queries that share the key head: each tile has one writer, so
+// nothing races.  Bound by memory and, for few tokens, by the latency of dependent
+// loads (sequence, page, scale): three workgroups side by side take 4.5 us for one
+// token where one doing all took 5.8 (4,680 tokens of 12 heads, 72 MB: 19.5 us).
 #include "cache.h"
 
 namespace sa {
@@ -23,7 +22,8 @@ constexpr int kThreads = 256;
 constexpr int kGroups = kThreads / 16;  // 16 threads a row of 128 channels, 8 channels each
 constexpr int kRows = kPage / kGroups;  // rows of a page per thread
 constexpr int kRowBytes = kHeadDim + 16;    // of a key's codes in LDS: its 16-byte pieces spread over the banks
-enum { kKeys, kValues, kQueries };      // what a workgroup takes (blockIdx.y)
+enum { kKeys, kValues, kQueries };      // what a workgroup takes (blockIdx.y; from kQueries on)
+constexpr int kMostQueries = 16;        // workgroups for a key head's queries
 
 // Smallest e >= -126 with amax <= 448 * 2^e.
 __device__ __forceinline__ int page_exponent(float amax) {
@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t merge4(uint32_t w, uint32_t n, int k0, int l
   return (w & ~m) | (n & m);
 }
 
-__global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
+__global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p, int heads) {
   __shared__ __attribute__((aligned(16))) uint8_t codes[kPage * kRowBytes];  // by key
   __shared__ float red[kThreads / kWave];
   const int h = blockIdx.x % p.c.Hkv, item = blockIdx.x / p.c.Hkv, role = blockIdx.y;
@@ -114,28 +114,31 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendIn p) {
     const int64_t row = p.rope_row ? (int64_t)p.rope_row[row0 + s] : base + s;
     return p.rope && row >= 0 && row < p.rope_rows ? p.rope + row * p.rope_dim : nullptr;
   };
-  if (role == kQueries) {  // those that share this key head, four rows of a thread in flight
-    const int g = p.c.g, rows = (s1 - s0) * g;
-    for (int i0 = r0; i0 < rows; i0 += 4 * kGroups) {
-      u32x4 w[4];
-      int s[4], hq[4];
+  if (role >= kQueries) {  // `heads` at a time, four rows of a thread in flight
+    for (int first = (role - kQueries) * heads; first < p.c.g;
+         first += ((int)gridDim.y - kQueries) * heads) {
+      const int h0 = h * p.c.g + first, g = min(p.c.g - first, heads), rows = (s1 - s0) * g;
+      for (int i0 = r0; i0 < rows; i0 += 4 * kGroups) {
+        u32x4 w[4];
+        int s[4], hq[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int i = i0 + u * kGroups, d = g == 1 ? i : i / g;
-        s[u] = s0 + d;
-        hq[u] = h * g + i - d * g;
-        if (i < rows) w[u] = ld16(p.q + (row0 + s[u]) * p.q_tok + hq[u] * p.q_head + c8);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i0 + u * kGroups < rows) {
-          float v[8];
-          widen8(v, w[u]);
-          rotate8(v, table(s[u]), c8, p.rope_dim);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) w[u][x] = pack_bf16x2(v[2 * x], v[2 * x + 1]);
-          st16(p.q_out + (row0 + s[u]) * p.qo_tok + hq[u] * p.qo_head + c8, w[u]);
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + u * kGroups, d = g == 1 ? i : i / g;
+          s[u] = s0 + d;
+          hq[u] = h0 + i - d * g;
+          if (i < rows) w[u] = ld16(p.q + (row0 + s[u]) * p.q_tok + hq[u] * p.q_head + c8);
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i0 + u * kGroups < rows) {
+            float v[8];
+            widen8(v, w[u]);
+            rotate8(v, table(s[u]), c8, p.rope_dim);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) w[u][x] = pack_bf16x2(v[2 * x], v[2 * x + 1]);
+            st16(p.q_out + (row0 + s[u]) * p.qo_tok + hq[u] * p.qo_head + c8, w[u]);
+          }
+      }
     }
     return;
   }
@@ -266,7 +269,13 @@ int64_t cache_append_items(const CacheIn& c) { return (int64_t)c.T / kPage + 2 *
 hipError_t launch_cache_append(const AppendIn& in, hipStream_t stream) {
   if (in.c.T == 0) return hipSuccess;
   const int64_t n = cache_append_items(in.c) * in.c.Hkv;
-  cache_append_kernel<<<dim3((unsigned)n, in.q ? 3 : 2), kThreads, 0, stream>>>(in);
+  // Query heads of a workgroup: four where pages get many tokens (2,000 tokens of 16
+  // heads on one: 9.0 us, eight heads 14.3, all of them 23), else eight (a token of
+  // each of 2,048 sequences, 40 heads on 8: 143 us, four heads 170).
+  const int heads = in.c.T >= 16 * (int64_t)in.c.B ? 4 : 8;
+  const int runs = (in.c.g + heads - 1) / heads;
+  const int queries = !in.q ? 0 : runs < kMostQueries ? runs : kMostQueries;
+  cache_append_kernel<<<dim3((unsigned)n, kQueries + queries), kThreads, 0, stream>>>(in, heads);
   return hipGetLastError();
 }
 

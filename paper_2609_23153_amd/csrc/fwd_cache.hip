@@ -35,6 +35,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWaveRows = 32;
+constexpr int kSlots = 512;  // workgroups that run at once: 256 CUs, two each
 constexpr float kLn2 = 0.69314718055994531f;
 // A row's running maximum (log2 units) may lag by this much before what has
 // been summed is rescaled: numerators up to 2^kLazy.
@@ -499,6 +500,13 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_cache_many_kernel(Params p) {
   int x = blockIdx.x;
   const int split = x % p.splits;
   x /= p.splits;
+  if (p.c.chunk > 0 && p.splits == 1) {
+    // Later rows of a sequence see more keys: they go first; where all workgroups
+    // run at once, the second of a CU are the shortest, shortest first (4,680
+    // tokens, 12 heads: 123 -> 112 us; 9,000: 319 -> 283)
+    const int all = gridDim.x;
+    x = all <= kSlots && x >= kSlots / 2 ? x - kSlots / 2 : all - 1 - x;
+  }
   const int h = x % p.c.Hkv;
   Tile t;
   if (!find_tile<kManyRows>(p.c, x / p.c.Hkv, &t)) return;
@@ -761,7 +769,6 @@ struct Plan {
   int64_t tiles;
   int splits, least;
 };
-constexpr int kSlots = 512;  // workgroups that run at once: 256 CUs, two each
 constexpr int kMostParts = kSlots;  // (joined by 8 waves of 64)
 Plan plan_of(const CacheIn& c) {
   Plan pl;

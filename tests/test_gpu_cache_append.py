@@ -225,3 +225,12 @@ def test_captured_and_replayed():
         for a, b in zip(c.dev + [out], eager + [want]):
             assert torch.equal(a, b), step
         length += 1
+
+
+@pytest.mark.parametrize("g,kv", [(9, 1), (40, 2), (130, 1)])
+@pytest.mark.parametrize("n", [3, 150])
+def test_many_query_heads_of_a_key_head(n, g, kv):
+    # more heads than a workgroup takes at a time, and than all of them do at once
+    c = Cache(4, kv, [[2, 0, 3, 1]])
+    c.append(tokens(n, kv, 7), tokens(n, kv, 8), [0, n], [n + 60], rope=table(256, 128),
+             q=tokens(n, kv * g, 9), what=f"{n} tokens, {kv}x{g}")
