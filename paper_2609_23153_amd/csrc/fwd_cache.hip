@@ -17,7 +17,7 @@
 //              waves of a workgroup take pages in turn, straight into
 //              registers, the next page's while one is worked on, and merge
 //              their softmax states through LDS.  One token over 524,288 (40
-//              heads on 8): 170 us, 6.3 TB/s of the cache's bytes
+//              heads on 8): 168 us, 6.4 TB/s of the cache's bytes
 //   many rows  bound by the matrix cores and the vector work beside them, which
 //              overlap little; four waves of 32 rows share every page through
 //              LDS.  4,680 tokens over 32,760 (12 heads): 0.92 ms, 1,020 TFLOP/s

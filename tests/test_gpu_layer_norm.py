@@ -182,8 +182,9 @@ def test_in_place_equals_out_of_place_and_repeats_bit_for_bit():
 
 def test_larger_than_the_caches_equals_its_parts():
     # rows that are kept out of the caches (over 512 MB) against the same rows a
-    # part at a time; fp32 and bf16, whole and with a padded row
-    for dtype, rows, cols, pad in ((torch.bfloat16, 14000, 10240, 0), (torch.float32, 9001, 8200, 8)):
+    # part at a time; fp32 and bf16, whole and with a padded row, aligned or not
+    for dtype, rows, cols, pad in ((torch.bfloat16, 14000, 10240, 0), (torch.float32, 9001, 8200, 8),
+                                    (torch.bfloat16, 30000, 5120, 3), (torch.bfloat16, 1200001, 128, 1)):
         g = torch.Generator(device=DEV).manual_seed(rows)
         rnd = lambda *s: torch.randn(*s, generator=g, device=DEV)
         x, dy = (rnd(rows, cols + pad).to(dtype)[:, :cols] for _ in range(2))
