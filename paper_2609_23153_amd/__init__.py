@@ -198,9 +198,9 @@ def _tile_desc(cnt, seqlen, block):
 
 
 def _stream(t):
-    if t.is_cuda:
-        return torch._C._cuda_getCurrentRawStream(t.device.index)
-    return torch.cuda.current_stream(t.device).cuda_stream
+    if not t.is_cuda:
+        raise ValueError("the tensors must be on a GPU")
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def _ptr(t):

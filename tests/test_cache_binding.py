@@ -1,0 +1,58 @@
+"""The Python side of the cache and norm calls on the host: what reaches the C
+ABI, and that a refusal names what is wrong (no GPU: the library is replaced by
+a recorder, or the call ends at the tensors' device)."""
+import pytest
+import torch
+
+import paper_2609_23153_amd as sa
+import test_abi_operators as T
+
+
+class Recorder:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 16 if name.endswith("_size") else 0
+        return call
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    lib = Recorder()
+    monkeypatch.setattr(sa, "library", lambda: lib)
+    monkeypatch.setattr(sa, "_stream", lambda t: 0)
+    return lib.calls
+
+
+def norm_args():
+    return dict(x=torch.zeros(4, 8)), dict(dy=torch.zeros(4, 8), x=torch.zeros(4, 8),
+                                           mean=torch.zeros(4), rstd=torch.ones(4))
+
+
+def test_tensors_off_the_gpu_are_refused():
+    # nothing may reach a kernel with a host address
+    args = T.cache_args()
+    fwd, bwd = norm_args()
+    q = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    pool = {n: t for n, t in args.items() if n not in ("k", "v")}
+    for call, kw in ((sa.sparse_attn_cache_append, args), (sa.sparse_attn_fwd_cache, dict(pool, q=q)),
+                     (sa.sparse_attn_layer_norm, fwd), (sa.sparse_attn_layer_norm_bwd, bwd),
+                     (sa.sparse_attn_quant_rows_fp8, dict(x=q[:, 0]))):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call(**kw)
+
+
+@pytest.mark.parametrize("bad", T.BAD_CACHE_TENSORS)
+def test_refusals_of_the_cache_name_the_tensor(recorded, bad):
+    # (by their own checks: the device is looked at last)
+    args = T.cache_args()
+    args.update(bad)
+    with pytest.raises(ValueError, match="|".join(bad)):
+        sa.sparse_attn_cache_append(**args)
+    del args["k"], args["v"]
+    with pytest.raises(ValueError, match="|".join(bad)):
+        sa.sparse_attn_fwd_cache(torch.zeros(6, 8, 128, dtype=torch.bfloat16), **args)
+    assert not [c for c in recorded if not c[0].endswith("_size")]
