@@ -444,7 +444,7 @@ typedef struct {
  *           operation rounded by itself.  A token whose row lies outside the
  *           table is not rotated
  *  rope_row int32 [T]: the table's row of every packed token, or NULL: its
- *           position in its sequence
+ *           position in its sequence; not read without a table
  *  q, q_out bf16 [T][heads][128] via q_stride and o_stride, or both NULL: the
  *           queries, rotated alike (copied without a table) and rounded to
  *           bf16; q_out may be q (then o_stride == q_stride)

@@ -602,8 +602,9 @@ def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=
     sequence's pages of 64 tokens, q_start int32 [B + 1] its packed rows,
     kv_len int32 [B] its tokens after the call.  rope fp32 [rows, r / 2, 2]
     rotates the first r channels of the keys, by position or by rope_row int32
-    [T], and of the queries q bf16 [T, heads, 128] if given.  Returns the
-    rotated queries (q_out, which may be q), or None without q."""
+    [T] (of no effect without rope), and of the queries q bf16 [T, heads, 128]
+    if given.  Returns the rotated queries (q_out, which may be q), or None
+    without q."""
     dev = k.get_device()
     if _elsewhere(dev):
         with torch.cuda.device(dev):
@@ -633,8 +634,6 @@ def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=
         rows, dim = rope.shape[0], 2 * rope.shape[1]
         cs = _arr(rope, "rope", torch.float32, dev, rows * dim)
     if rope_row is not None:
-        if rope is None:
-            raise ValueError("rope_row without rope")
         row = _arr(rope_row, "rope_row", torch.int32, dev, T)
     desc = _CACHE_DESC.pack(batch, heads, kv, 128, T, num, most, stride, q0, q1, k0, k1, v0, v1, o0,
                             o1, 0.0, 0, 0)

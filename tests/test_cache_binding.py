@@ -27,6 +27,26 @@ def recorded(monkeypatch):
     return lib.calls
 
 
+def test_append_takes_rows_without_a_table(recorded):
+    args = T.cache_args()
+    rows = torch.zeros(6, dtype=torch.int32)
+    assert sa.sparse_attn_cache_append(**args, rope_row=rows) is None
+    q = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    assert sa.sparse_attn_cache_append(**args, rope_row=rows, q=q, q_out=q) is q
+    for name, a in recorded:
+        assert name == "sparse_attn_cache_append"
+        assert a[3] is None and a[4] == a[5] == 0      # no table
+    assert recorded[1][1][7] == recorded[1][1][8] == q.data_ptr()
+
+
+@pytest.mark.parametrize("rows", [torch.zeros(5, dtype=torch.int32), torch.zeros(6, dtype=torch.int64),
+                                  torch.zeros(12, dtype=torch.int32)[::2]])
+def test_rows_without_a_table_are_checked_alike(recorded, rows):
+    with pytest.raises(ValueError, match="rope_row"):
+        sa.sparse_attn_cache_append(**T.cache_args(), rope_row=rows)
+    assert not recorded
+
+
 def norm_args():
     return dict(x=torch.zeros(4, 8)), dict(dy=torch.zeros(4, 8), x=torch.zeros(4, 8),
                                            mean=torch.zeros(4), rstd=torch.ones(4))
