@@ -476,7 +476,8 @@ size_t sparse_attn_fwd_cache_workspace_size(const sparse_attn_cache_desc* desc);
  * of pages outside the pool:
  *   o_t = sum_u softmax_u(tau q_t.k_u) v_u,  lse_t = log sum_u exp(tau q_t.k_u)
  * on the dequantised keys and values; a query that sees no key gets o = 0 and
- * lse = -inf.  Products accumulate in fp32; queries, keys and values enter
+ * lse = -inf, one that sees keys and holds a NaN gets NaN for both (no other
+ * row changes).  Products accumulate in fp32; queries, keys and values enter
  * exactly, the probabilities rounded to 8 significant bits, the row sums
  * unrounded.  A sequence's cached
  * tokens must be finite in every page that some query of the call sees a key

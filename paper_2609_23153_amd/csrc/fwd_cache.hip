@@ -285,8 +285,9 @@ __device__ __forceinline__ void store4(uint16_t* o, const float (&x)[4], float i
   *reinterpret_cast<u32x2*>(o) = v;
 }
 
+// (a sum that is NaN stays NaN)
 __device__ __forceinline__ float lse_of(float m, float l) {
-  return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  return l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // Channels 32 dt .. +31 of the wave's rows, their sums l over all keys of the
