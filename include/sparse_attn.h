@@ -404,8 +404,9 @@ int sparse_attn_linear_w8a8(const uint8_t* xq, const float* sx, int64_t ldx, con
  *  num_pages   pages P >= 1 of the pool
  *  max_pages   entries of a page-table row, 1 <= max_pages < 2^24
  *  pages_stride  elements from one page-table row to the next (>= max_pages)
- *  *_stride    element strides of (token, head), channels contiguous; rows that
- *              are written must not overlap
+ *  *_stride    element strides of (token, head), multiples of 8, channels
+ *              contiguous; rows that are written must not overlap: a step of the
+ *              larger stride is past all rows along the smaller one
  *  softmax_scale, causal_chunk, causal_window  as in sparse_attn_desc (the
  *              position of a token in its sequence decides its chunk)
  * Device tensors of a cache, contiguous but for the table's rows:

@@ -426,9 +426,16 @@ bool strides2_ok(const int64_t st[2]) {
   return st[0] >= 0 && (st[0] & 7) == 0 && st[1] >= 0 && (st[1] & 7) == 0;
 }
 
-// Rows of 128 channels that are written must not lie on each other.
+// Rows of 128 channels that are written must not lie on each other: one axis's rows
+// stand apart, and a step along the other one is past all of them.
 bool out_strides_ok(const int64_t st[2], int64_t tokens, int64_t heads) {
-  return strides2_ok(st) && (tokens <= 1 || st[0] >= 128) && (heads <= 1 || st[1] >= 128);
+  if (!strides2_ok(st)) return false;
+  const bool by_token = st[0] >= st[1];  // the larger step is a token's
+  const int64_t near = by_token ? heads : tokens, far = by_token ? tokens : heads;
+  const int64_t step = by_token ? st[1] : st[0], leap = by_token ? st[0] : st[1];
+  if (near <= 1) return far <= 1 || leap >= 128;
+  if (far <= 1) return step >= 128;
+  return step >= 128 && (leap - 128) / step >= near - 1;
 }
 
 int check_cache_desc(const sparse_attn_cache_desc* d, sa::CacheIn* c) {
