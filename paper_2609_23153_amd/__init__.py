@@ -566,7 +566,7 @@ def _cache_pool(dev, k8, sk, v8, sv, pages, q_start, kv_len):
     """(pages of the pool, key heads, sequences, table entries, table stride)
     and the tensors' addresses."""
     shape = k8.shape
-    if len(shape) != 3 or shape[2] != 8192:
+    if len(shape) != 3 or shape[1] < 1 or shape[2] != 8192:
         raise ValueError("k8 and v8 must be uint8 [pages, kv_heads, 8192]")
     num, kv, _ = shape
     if pages.dim() != 2 or pages.dtype is not torch.int32 or pages.get_device() != dev:
@@ -611,7 +611,7 @@ def sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope=
             return sparse_attn_cache_append(k, v, k8, sk, v8, sv, pages, q_start, kv_len, rope,
                                             rope_row, q, q_out)
     (num, kv, batch, most, stride), cache = _cache_pool(dev, k8, sk, v8, sv, pages, q_start, kv_len)
-    T = k.shape[0]
+    T = k.shape[0] if k.dim() else 0
     k0, k1 = _packed(k, "k", dev, kv, T)
     v0, v1 = _packed(v, "v", dev, kv, T)
     heads, q0, q1, o0, o1, qp, op = kv, 0, 0, 0, 0, None, None

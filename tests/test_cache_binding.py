@@ -76,3 +76,16 @@ def test_refusals_of_the_cache_name_the_tensor(recorded, bad):
     with pytest.raises(ValueError, match="|".join(bad)):
         sa.sparse_attn_fwd_cache(torch.zeros(6, 8, 128, dtype=torch.bfloat16), **args)
     assert not [c for c in recorded if not c[0].endswith("_size")]
+
+
+def test_a_pool_without_key_heads_and_scalars_are_refused(recorded):
+    args = T.cache_args()
+    none = dict(args, k8=args["k8"][:, :0], v8=args["v8"][:, :0], sk=args["sk"][:, :0], sv=args["sv"][:, :0])
+    q = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="k8"):
+        sa.sparse_attn_cache_append(**dict(none, k=args["k"][:, :0], v=args["v"][:, :0], q=q))
+    with pytest.raises(ValueError, match="k8"):
+        sa.sparse_attn_fwd_cache(q, **{n: t for n, t in none.items() if n not in ("k", "v")})
+    with pytest.raises(ValueError, match="k must be"):
+        sa.sparse_attn_cache_append(**dict(args, k=args["k"][0, 0, 0]))
+    assert not recorded
