@@ -21,9 +21,9 @@ def _gpu():
 
 
 @pytest.mark.parametrize("chunk,window", [(0, 0), (1, 0), (1, 40), (64, 2), (1000, 1)])
-@pytest.mark.parametrize("n", [1, 12, 150])              # few rows, many rows
+@pytest.mark.parametrize("n", [1, 150])                  # few rows, many rows
 @pytest.mark.parametrize("pages", [5, 40])               # whole, in parts
-@pytest.mark.parametrize("past", [1, 10, 139, 4680, (1 << 31) - 5000])
+@pytest.mark.parametrize("past", [1, 139, (1 << 31) - 5000])
 def test_length_past_the_table(past, pages, n, chunk, window):
     held = 64 * pages
     k8, sk, v8, sv, table = make_cache([held, 30], 2, 41)
@@ -36,7 +36,7 @@ def test_length_past_the_table(past, pages, n, chunk, window):
                              causal=(chunk, window) if chunk else None)
     compare(o, lse, q, (k8, sk, v8, sv), table, start, lengths, chunk, window,
             what=f"{n} rows, {held} + {past} tokens")
-    if chunk == 1 and window and past >= 139 and n <= 12:    # every window is past the table
+    if chunk == 1 and window and past >= 139 and n == 1:     # every window is past the table
         assert bool(lse[:n].isneginf().all()) and not bool(o[:n].any())
     if window == 0 and past >= n:                            # every row sees all that is held
         want, want_lse = sa.sparse_attn_fwd_cache(q, k8, sk, v8, sv, ints(table), ints(start), ints([held, 30]))
