@@ -490,6 +490,9 @@ size_t sparse_attn_fwd_cache_workspace_size(const sparse_attn_cache_desc* desc);
  * Rows of o and lse outside every sequence are left as they are.  T == 0
  * launches nothing.  Deterministic; a row's last bits depend on how its keys
  * are cut into parts, which the descriptor's sizes and its own length decide.
+ * The sizes also choose one kernel for the whole call, for the average sequence:
+ * long prompts beside single tokens, and sequences many times longer than the
+ * others, are faster in calls of their own.
  * Errors: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE. */
 int sparse_attn_fwd_cache(const sparse_attn_cache_desc* desc, const void* q, const uint8_t* k8,
                           const float* sk, const uint8_t* v8, const float* sv,

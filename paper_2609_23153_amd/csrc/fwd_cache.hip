@@ -20,7 +20,7 @@
 //              heads on 8): 168 us, 6.4 TB/s of the cache's bytes
 //   many rows  bound by the matrix cores and the vector work beside them, which
 //              overlap little; four waves of 32 rows share every page through
-//              LDS.  4,680 tokens over 32,760 (12 heads): 0.92 ms, 1,020 TFLOP/s
+//              LDS.  4,680 tokens over 32,760 (12 heads): 0.91 ms, 1,030 TFLOP/s
 //              (a large bf16 library product: 1,380), matrix cores busy 48% of
 //              the cycles, vector units 46%, LDS 36%, at 2.0 GHz
 // Long key ranges are cut over workgroups when there are few rows: partial
@@ -178,8 +178,7 @@ __device__ __forceinline__ void mask_scores(const Wave& w, int start, int keys, 
     }
 }
 
-// Raises the rows' maxima to a page's where they lag by more than kLazy, and
-// brings what has been summed to the new ones.
+// The lane's largest score of a page.
 __device__ __forceinline__ float page_max(const f32x16 (&s)[2]) {
   float mx = s[0][0];
 #pragma unroll
@@ -188,6 +187,8 @@ __device__ __forceinline__ float page_max(const f32x16 (&s)[2]) {
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[rt][r]);
   return mx;
 }
+// Raises the rows' maxima to a page's where they lag by more than kLazy, and
+// brings what has been summed to the new ones.
 __device__ __forceinline__ void raise_max(Wave& w, float mx, float scale_log2) {
   mx = pair_max32(mx) * scale_log2;
   // a row without keys so far takes any maximum; -inf is above nothing
@@ -784,12 +785,20 @@ __global__ __launch_bounds__(W == 1 ? kThreads : W * kWave) void fwd_cache_join_
   if (lane == 0 && p.lse) p.lse[row] = lse_of(m, l);
 }
 
-// How the work is cut.  Few rows a sequence go to the kernel that is bound by
-// the cache's bytes.  Where its tiles do not fill the slots, a range is cut until
-// they do, or until there is one workgroup a CU where that leaves parts of fewer
-// than eight pages (a part's start and end cost about as much as two pages; one
-// token over 32,768 of 4 heads: 12.4 us, 16.7 with all slots filled); a part has
-// at least one page a wave, four where the tiles alone fill the slots.
+// How the work is cut: one kernel and one number of parts for a call, from the
+// averages of its sizes (lengths are on the device).  Up to 32 rows a sequence, a
+// wave's tile, go to the kernel that is bound by the cache's bytes; past that the
+// other one reads a page once for four such tiles, but cuts no range while tiles
+// fill the chip.  Sequences of one length are served much alike on both sides (64 of
+// 4,096 keys, 40 heads on 8: 6 tokens each, 30 rows, 123 us; 7 tokens 161; 8 tokens
+// 112); of ragged ones the longest then runs on alone (16 to 16,384 keys: 107, 357
+// and 286 us), and so does one that is much longer than the average on either side
+// (1,023 sequences of 100 keys and one of 524,288: 2.8 ms).
+// Where its tiles do not fill the slots, a range is cut until they do, or until
+// there is one workgroup a CU where that leaves parts of fewer than eight pages (a
+// part's start and end cost about as much as two pages; one token over 32,768 of 4
+// heads: 12.4 us, 16.7 with all slots filled); a part has at least one page a wave,
+// four where the tiles alone fill the slots.
 // Short tables are not cut: one token over 24 pages of 12 heads takes 13.0 us in
 // a stream of calls, 30 alone and 10.6 in a captured graph whole, 15.7, 29 and
 // 9.5 in parts; over 48 pages 16.5, 36 and 17, in parts 15.7, 30 and 9.8.

@@ -20,7 +20,7 @@ namespace sa {
 namespace {
 
 // 16 bytes at any element's address; ONCE: data too large for the caches, which
-// it is then kept out of.
+// it is then kept out of (rows of whole pieces alone).
 template <typename T>
 struct Any16;
 template <>
@@ -385,14 +385,16 @@ __global__ __launch_bounds__(kWave* kRedRuns) void layer_norm_reduce_kernel(cons
 }
 
 // Threads per row.  Up to 128 channels, four rows share a wave (75,600 x 96 bf16:
-// 14 us, a wave a row 26).  Forward: a wave alone needs no barrier and serves rows
+// 13 us, a wave a row 26).  Forward: a wave alone needs no barrier and serves rows
 // up to 2048 channels; longer ones take four or eight.  Backward: four from 1024
 // channels on, so that fewer workgroups, and with them fewer partial gradients,
 // keep as many waves busy (1,554 x 1,531 fp32: 777 one-wave teams a group 26 us
-// with the sum of the partials, 128 of four waves 18.5); eight from 6144 on, as a
+// with the sum of the partials, 128 of four waves 18.4); eight from 6144 on, as a
 // thread of four would hold more than 24 elements and spill (20,000 x 9,000 bf16:
 // 308 us, 244 with eight); sixteen from 12288 on, without the next row's loads in
-// flight (6,000 x 16,384 fp32: eight 450 us, sixteen 296).
+// flight (6,000 x 16,384 fp32: eight 450 us, sixteen 296).  Those have 128 registers;
+// where rows are not whole pieces, 8 (bf16) to 10 (fp32) of them spill (6,000 x 16,384
+// bf16: 178 us, 16,380: 196).
 int team_of(int64_t cols, bool backward) {
   if (cols <= 128) return 16;
   if (cols <= 1024) return 64;
@@ -465,9 +467,9 @@ void run_team(const In& in, float* part, hipStream_t stream) {
 // rows lose up to a third (40,000 x 5,119: forward 185 us, backward 308; 5,120: 154
 // and 232), fp32 rows nothing.  An element a load was slower for most (75,600 x 701
 // forward 71 us, 46 by pieces; 20,000 x 9,001 backward 496, 308), 10% faster for the
-// backward of some (5,119: 279).  More than twice
-// what the last-level cache holds (256 MB) is kept out of the caches (75,600 x
-// 5,120 bf16: forward 321 -> 301 us, backward 460 -> 417); less is left in them,
+// backward of some (5,119: 279).  Rows of whole pieces, where they are more than
+// twice what the last-level cache holds (256 MB), are kept out of the caches (75,600
+// x 5,120 bf16: forward 321 -> 301 us, backward 460 -> 417); less is left in them,
 // mostly for the call that reads the result (4,680 rows: 19.5 us, kept out 22.6).
 template <typename T, typename In>
 void run_rows(const In& in, float* part, int tensors, hipStream_t stream) {
