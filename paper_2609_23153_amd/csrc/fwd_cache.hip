@@ -237,7 +237,7 @@ __device__ __forceinline__ Half numerators(float scale_log2, float ref, const f3
 
 // The row sum has three levels, so that its error does not grow with the number of
 // keys (term after term, equal scores drift: lse off by 8e-4 at 131,072 keys, three
-// levels 1e-6): a page's numerators, up to 64 pages, all of them.  The last step is
+// levels 2e-6): a page's numerators, up to 64 pages, all of them.  The last step is
 // made where 64 more pages are looked up and costs nothing (a compensated sum of
 // pages: 0.7% of frames over a long cache).
 __device__ __forceinline__ void fold_sum(Wave& w) {

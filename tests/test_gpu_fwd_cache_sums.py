@@ -108,3 +108,13 @@ def test_ranges_in_parts(rows):
     for size in SIZES:
         o, lse = sa.sparse_attn_fwd_cache(query(rows, 1, size), *pool, pages, ints([0, rows]), ints([n]))
         check(o, lse, size, n, f"{n} keys in parts, {rows} rows")
+
+
+def test_pages_one_by_one():
+    # a table that misses a page takes every page by itself
+    n = 131072
+    pool, pages = one_key(n, 1), ints(np.arange(n // 64)[None])
+    pages[0, 1500] = -1
+    for size in SIZES:
+        o, lse = sa.sparse_attn_fwd_cache(query(512, 64, size), *pool, pages, ints([0, 512]), ints([n]))
+        check(o, lse, size, n - 64, f"{n} keys, a page missing")
